@@ -40,8 +40,10 @@
  *     enqueued.  MICS_ERR_HIP reports the status of the failed launch call
  *     itself (an earlier, unrelated HIP error of the thread is neither reported
  *     nor cleared); every entry point issues a single launch, except the
- *     coalesced ones, which issue one per 48 to 96 tensors and may have
- *     enqueued earlier launches when a later one fails.
+ *     coalesced ones, which issue one per 48 to 96 tensors, backward passes
+ *     that sum over rows (two, or three with very long rows) and log
+ *     probabilities of few long rows (two): these may have enqueued earlier
+ *     launches when a later one fails.
  *   - Return value: MICS_OK or a negative MICS_ERR_*; mics_last_error() gives
  *     the text for the calling thread's most recent failure.
  *   - bf16 values travel as uint16_t bit patterns (upper half of a binary32).
@@ -271,6 +273,156 @@ int mics_reduce_scatter_accum_coalesced(float* acc, const uint16_t* const* grads
 int mics_reduce_scatter_accum_coalesced_typed(float* acc, const void* const* grads,
                                               const mics_segment* segs, int n_segs, int p,
                                               int accumulate, int grad_dtype, void* stream);
+
+/*
+ * Operators of a transformer layer's training step between the parameter gather and the gradient
+ * reduction: what a rank runs on the gathered parameters, and what leaves the gradients that
+ * mics_reduce_scatter_accum reads.  The paper's models are such layers (Table 1); it does not describe
+ * these operators.
+ *
+ * Conventions, beyond those above
+ *   - A matrix is `rows` rows of `cols` elements of `dtype`; parameter vectors are of `param_dtype`,
+ *     their gradients of `grad_dtype` (MICS_DTYPE_* each, in any combination).
+ *   - `strides`: HOST array of the row strides, in elements and at least `cols`, in the order of the
+ *     matrix arguments as the entry point lists them; NULL = every matrix is packed (stride cols).
+ *   - 1 <= cols, vocab <= 2^24.  rows may be 0: gradients of parameters are then written as zeros,
+ *     and nothing else is.
+ *   - Buffers need only be aligned to their elements; rows that begin on 16 bytes are fastest.
+ *   - A result matrix may be an input matrix of the same address and stride.  Matrices of one stride may
+ *     lie between each other's rows.  No other overlap of a result is allowed (checked).
+ *   - Everything is computed in binary32 and rounded to nearest even once, when it is stored.
+ *     Sums are formed in an order that depends on the sizes alone: results are reproducible.
+ *   - `workspace`: caller-owned scratch of at least the stated bytes, 8-byte aligned, its contents of no
+ *     meaning before or after; one may serve any number of calls that are ordered by a stream.
+ */
+
+/*
+ * Dropout.  Element (row, col) of a call belongs to the 16-bit number `col mod 8` (low half of word 0
+ * first) of the block with counter offset + row * ceil(cols / 8) + col div 8 (mod 2^64) of
+ * Philox4x32-10 under the key `seed` (low 32 bits first); the counter's upper 64 bits are 0.  With
+ * T = min(65535, rint(65536 * drop)) the element is kept if its number is at least T, and
+ *     D(v) = kept ? v * (65536 / (65536 - T)) : +0,
+ * so that D has the mean v exactly; `drop` is realised in steps of 2^-16.  No mask is stored: the
+ * backward pass takes the same drop, seed and offset.  0 <= drop < 1; 0 keeps everything.
+ * mics_dropout_counters: how many counters a call uses, i.e. how far apart the offsets of calls with the
+ * same seed have to be: rows * ceil(cols / 8).
+ */
+uint64_t mics_dropout_counters(size_t rows, size_t cols);
+
+/*
+ *     out = residual + D(x + bias)
+ *   strides    out, x, residual
+ *   bias       cols, may be NULL (0); residual may be NULL (0)
+ */
+int mics_bias_dropout_add(void* out, const void* x, const void* bias, const void* residual,
+                          size_t rows, size_t cols, const size_t* strides, float drop,
+                          uint64_t seed, uint64_t offset, int dtype, int param_dtype, void* stream);
+
+/*
+ *     dx = D(dout),   dbias[c] = sum over the rows of D(dout)[., c], before it is rounded
+ * (the residual's gradient is dout).
+ *   strides    dx, dout
+ *   dbias      cols, may be NULL; then no workspace is needed
+ */
+int mics_bias_dropout_add_backward(void* dx, void* dbias, const void* dout, size_t rows,
+                                   size_t cols, const size_t* strides, float drop, uint64_t seed,
+                                   uint64_t offset, int dtype, int grad_dtype, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* Workspace of the backward passes that sum over rows.  0 on bad arguments. */
+size_t mics_column_workspace_bytes(size_t rows, size_t cols);
+
+/*
+ * Layer norm:  mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),
+ *     y = (x - mean) * rstd * weight + bias
+ *   strides        y, x
+ *   mean, rstd     rows fp32 each, written for the backward pass; may be NULL
+ *   weight, bias   cols, may be NULL (1 and 0)
+ */
+int mics_layer_norm(void* y, float* mean, float* rstd, const void* x, const void* weight,
+                    const void* bias, size_t rows, size_t cols, const size_t* strides, float eps,
+                    int dtype, int param_dtype, void* stream);
+
+/*
+ * With h = (x - mean) * rstd and g = dy * weight:
+ *     dx = rstd * (g - sum g / cols - h * (sum g * h / cols)),
+ *     dweight = sum over the rows of dy * h,   dbias = sum over the rows of dy
+ *   strides          dx, dy, x
+ *   mean, rstd       as the forward pass left them
+ *   dweight, dbias   cols, may be NULL
+ */
+int mics_layer_norm_backward(void* dx, void* dweight, void* dbias, const void* dy, const void* x,
+                             const float* mean, const float* rstd, const void* weight, size_t rows,
+                             size_t cols, const size_t* strides, int dtype, int param_dtype,
+                             int grad_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * mics_bias_dropout_add and mics_layer_norm in one pass:
+ *     s = residual + D(x + bias),   y = layer_norm(s; weight, norm_bias),   sum = s
+ * The norm takes s before it is rounded to `sum`.
+ *   strides                                  y, sum, x, residual
+ *   sum, mean, rstd, bias, residual, weight, norm_bias   may be NULL
+ */
+int mics_dropout_add_layer_norm(void* y, void* sum, float* mean, float* rstd, const void* x,
+                                const void* bias, const void* residual, const void* weight,
+                                const void* norm_bias, size_t rows, size_t cols,
+                                const size_t* strides, float drop, uint64_t seed, uint64_t offset,
+                                float eps, int dtype, int param_dtype, void* stream);
+
+/*
+ * Its backward pass:  ds = the dx of mics_layer_norm_backward(dy, sum, ...) + dsum,
+ *     dresidual = ds,   dx = D(ds),   dbias = sum over the rows of D(ds),   dweight, dnorm_bias
+ * with D taken and summed before ds is rounded.
+ *   strides    dx, dresidual, dy, dsum, sum
+ *   dsum       gradient that reaches `sum` by other ways, may be NULL (0)
+ *   dresidual, dbias, dweight, dnorm_bias   may be NULL
+ */
+int mics_dropout_add_layer_norm_backward(void* dx, void* dresidual, void* dbias, void* dweight,
+                                         void* dnorm_bias, const void* dy, const void* dsum,
+                                         const void* sum, const float* mean, const float* rstd,
+                                         const void* weight, size_t rows, size_t cols,
+                                         const size_t* strides, float drop, uint64_t seed,
+                                         uint64_t offset, int dtype, int param_dtype,
+                                         int grad_dtype, void* workspace, size_t workspace_bytes,
+                                         void* stream);
+
+/*
+ * Log probabilities of given tokens under softmax(logits), a row for each token:
+ *     lse = log sum exp logits,   logprob = logits[target] - lse,
+ *     entropy = - sum p log p  (0 where p is 0),
+ *     top_ids, top_logprobs: the top_k largest logits in descending order and their log probabilities,
+ *     the lower index first among equals (NaN counts as larger than all numbers).
+ * A negative target means none: logprob 0.  A target of vocab or more gives NaN.  Logits of -inf have
+ * probability 0; a row of nothing else has lse, logprob and top_logprobs -inf and entropy 0.  NaN or +inf
+ * among the logits makes the row's lse, logprob, entropy and top_logprobs NaN.
+ *   logprob, entropy, lse   rows fp32; entropy and lse may be NULL
+ *   top_ids, top_logprobs   rows * top_k, int64 and fp32; NULL with top_k = 0
+ *   targets                 rows int64, device
+ *   stride                  of the rows of logits
+ *   top_k                   0 <= top_k <= min(vocab, MICS_MAX_TOP)
+ *   workspace               mics_token_logprobs_workspace_bytes(rows, vocab, top_k), which is 0 unless rows
+ *                           are few and long; then a second launch joins the parts of each row
+ */
+#define MICS_MAX_TOP 64
+size_t mics_token_logprobs_workspace_bytes(size_t rows, size_t vocab, int top_k);
+int mics_token_logprobs(float* logprob, float* entropy, float* lse, int64_t* top_ids,
+                        float* top_logprobs, const void* logits, const int64_t* targets,
+                        size_t rows, size_t vocab, size_t stride, int top_k, int dtype,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradient of the logits, from those of logprob and entropy:
+ *     dlogits[j] = dlogprob * (1[j = target] - p[j]) - dentropy * p[j] * (log p[j] + entropy)
+ * dlogprob counts as 0 where the target is negative.  Rows that neither reaches, and rows of nothing but
+ * -inf, are written as zeros and not read; a target of vocab or more gives a row of NaN.
+ *   strides         dlogits, logits (dlogits may be logits)
+ *   lse, entropy    as the forward pass left them; entropy may be NULL without dentropy
+ *   dlogprob        rows fp32; dentropy: rows fp32, may be NULL (0)
+ */
+int mics_token_logprobs_backward(void* dlogits, const void* logits, const int64_t* targets,
+                                 const float* lse, const float* entropy, const float* dlogprob,
+                                 const float* dentropy, size_t rows, size_t vocab,
+                                 const size_t* strides, int dtype, void* stream);
 
 #ifdef __cplusplus
 }

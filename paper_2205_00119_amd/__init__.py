@@ -29,7 +29,12 @@ EXPORTS = (
     "mics_replica_average_adam_shard", "mics_reduce_scatter_accum_typed",
     "mics_adam_shard_typed", "mics_replica_average_adam_shard_typed",
     "mics_reduce_scatter_accum_coalesced_typed",
+    "mics_dropout_counters", "mics_column_workspace_bytes", "mics_token_logprobs_workspace_bytes",
+    "mics_bias_dropout_add", "mics_bias_dropout_add_backward", "mics_layer_norm", "mics_layer_norm_backward",
+    "mics_dropout_add_layer_norm", "mics_dropout_add_layer_norm_backward",
+    "mics_token_logprobs", "mics_token_logprobs_backward",
 )
+MICS_MAX_TOP = 64
 MICS_DTYPE_BF16, MICS_DTYPE_F16, MICS_DTYPE_F32 = 0, 1, 2
 
 
@@ -107,6 +112,27 @@ lib.mics_reduce_scatter_accum_typed.argtypes = [_vp, _vp, _sz, _sz, _i, _i, _i, 
 lib.mics_reduce_scatter_accum_typed.restype = _i
 
 
+_u64 = ctypes.c_uint64
+lib.mics_dropout_counters.argtypes = [_sz, _sz]
+lib.mics_dropout_counters.restype = _u64
+lib.mics_column_workspace_bytes.argtypes = [_sz, _sz]
+lib.mics_column_workspace_bytes.restype = _sz
+lib.mics_token_logprobs_workspace_bytes.argtypes = [_sz, _sz, _i]
+lib.mics_token_logprobs_workspace_bytes.restype = _sz
+lib.mics_bias_dropout_add.argtypes = [_vp] * 4 + [_sz, _sz, _vp, _f, _u64, _u64, _i, _i, _vp]
+lib.mics_bias_dropout_add_backward.argtypes = [_vp] * 3 + [_sz, _sz, _vp, _f, _u64, _u64, _i, _i, _vp, _sz, _vp]
+lib.mics_layer_norm.argtypes = [_vp] * 6 + [_sz, _sz, _vp, _f, _i, _i, _vp]
+lib.mics_layer_norm_backward.argtypes = [_vp] * 8 + [_sz, _sz, _vp, _i, _i, _i, _vp, _sz, _vp]
+lib.mics_dropout_add_layer_norm.argtypes = [_vp] * 9 + [_sz, _sz, _vp, _f, _u64, _u64, _f, _i, _i, _vp]
+lib.mics_dropout_add_layer_norm_backward.argtypes = [_vp] * 11 + [_sz, _sz, _vp, _f, _u64, _u64, _i, _i, _i, _vp, _sz, _vp]
+lib.mics_token_logprobs.argtypes = [_vp] * 7 + [_sz, _sz, _sz, _i, _i, _vp, _sz, _vp]
+lib.mics_token_logprobs_backward.argtypes = [_vp] * 7 + [_sz, _sz, _vp, _i, _vp]
+_LAYER_CALLS = ("bias_dropout_add", "bias_dropout_add_backward", "layer_norm", "layer_norm_backward", "dropout_add_layer_norm",
+                "dropout_add_layer_norm_backward", "token_logprobs", "token_logprobs_backward")
+for _name in _LAYER_CALLS:
+    getattr(lib, "mics_" + _name).restype = _i
+
+
 def _segments(segs) -> ctypes.Array:
     """(numel, shard_elems, src_offset, dst_offset) tuples -> C array of mics_segment."""
     arr = (mics_segment * len(segs))()
@@ -149,6 +175,7 @@ _marshal.bind(tuple(ctypes.cast(getattr(lib, "mics_" + name), _vp).value for nam
     "reduce_scatter_accum_coalesced", "reduce_scatter_accum_coalesced_typed", "replica_average", "adam_shard",
     "adam_shard_typed", "replica_average_adam_shard", "replica_average_adam_shard_typed")),
     _device, _raw_stream)
+_marshal.bind_layer(tuple(ctypes.cast(getattr(lib, "mics_" + name), _vp).value for name in _LAYER_CALLS))
 _marshal.bind_segment(mics_segment)
 
 
@@ -309,3 +336,132 @@ def mics_reduce_scatter_accum_typed(acc, grads: Sequence, elem_offset: int, coun
     _check(lib.mics_reduce_scatter_accum_typed(_dev_ptr(acc), _table(grads), elem_offset, count,
                                                len(grads), int(bool(accumulate)), grad_dtype,
                                                _stream(stream)))
+
+
+# The operators between the parameter gather and the gradient reduction.  A matrix is a packed tensor, a tensor of two
+# dimensions whose rows are as far apart as `strides` says, or an address; `strides` holds the row strides in elements of
+# the matrices in the order in which the call takes them, None: all are packed.
+
+def _strides(strides, n: int):
+    if strides is None:
+        return None
+    if len(strides) != n:
+        raise ValueError(f"expected {n} row strides, got {len(strides)}")
+    return (ctypes.c_size_t * n)(*[int(x) for x in strides])
+
+
+def _matrix(x, strides, k: int = 0):
+    if strides is not None and isinstance(x, torch.Tensor) and x.dim() == 2 and x.stride(1) == 1 and x.stride(0) == strides[k]:
+        return x.data_ptr()
+    return _dev_ptr(x)
+
+
+def mics_dropout_counters(rows: int, cols: int) -> int:
+    """Counters that a dropout call uses: how far apart the offsets of calls with one seed have to be."""
+    return lib.mics_dropout_counters(rows, cols)
+
+
+def mics_column_workspace_bytes(rows: int, cols: int) -> int:
+    """Workspace of the backward passes that sum over rows."""
+    return lib.mics_column_workspace_bytes(rows, cols)
+
+
+def mics_token_logprobs_workspace_bytes(rows: int, vocab: int, top_k: int = 0) -> int:
+    return lib.mics_token_logprobs_workspace_bytes(rows, vocab, top_k)
+
+
+def mics_bias_dropout_add(out, x, bias, residual, rows: int, cols: int, *, drop: float, seed: int, offset: int, dtype: int,
+                          param_dtype: int, strides=None, stream=None) -> None:
+    """out = residual + D(x + bias); strides: out, x, residual."""
+    if _done(_marshal.bias_dropout_add(out, x, bias, residual, rows, cols, strides, drop, seed, offset, dtype, param_dtype, stream)):
+        return
+    st = _strides(strides, 3)
+    _check(lib.mics_bias_dropout_add(_matrix(out, st, 0), _matrix(x, st, 1), _dev_ptr(bias), _matrix(residual, st, 2), rows, cols, st,
+                                     drop, seed, offset, dtype, param_dtype, _stream(stream)))
+
+
+def mics_bias_dropout_add_backward(dx, dbias, dout, rows: int, cols: int, *, drop: float, seed: int, offset: int, dtype: int,
+                                   grad_dtype: int, workspace=None, workspace_bytes: int = 0, strides=None, stream=None) -> None:
+    """dx = D(dout) and its column sums; strides: dx, dout."""
+    if _done(_marshal.bias_dropout_add_backward(dx, dbias, dout, rows, cols, strides, drop, seed, offset, dtype, grad_dtype, workspace,
+                                                workspace_bytes, stream)):
+        return
+    st = _strides(strides, 2)
+    _check(lib.mics_bias_dropout_add_backward(_matrix(dx, st, 0), _dev_ptr(dbias), _matrix(dout, st, 1), rows, cols, st, drop, seed,
+                                              offset, dtype, grad_dtype, _dev_ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def mics_layer_norm(y, mean, rstd, x, weight, bias, rows: int, cols: int, *, eps: float, dtype: int, param_dtype: int,
+                    strides=None, stream=None) -> None:
+    """Layer norm of every row; mean and rstd for the backward pass.  strides: y, x."""
+    if _done(_marshal.layer_norm(y, mean, rstd, x, weight, bias, rows, cols, strides, eps, dtype, param_dtype, stream)):
+        return
+    st = _strides(strides, 2)
+    _check(lib.mics_layer_norm(_matrix(y, st, 0), _dev_ptr(mean), _dev_ptr(rstd), _matrix(x, st, 1), _dev_ptr(weight), _dev_ptr(bias),
+                               rows, cols, st, eps, dtype, param_dtype, _stream(stream)))
+
+
+def mics_layer_norm_backward(dx, dweight, dbias, dy, x, mean, rstd, weight, rows: int, cols: int, *, dtype: int, param_dtype: int,
+                             grad_dtype: int, workspace, workspace_bytes: int, strides=None, stream=None) -> None:
+    """Gradients of rows, weight and bias; strides: dx, dy, x."""
+    if _done(_marshal.layer_norm_backward(dx, dweight, dbias, dy, x, mean, rstd, weight, rows, cols, strides, dtype, param_dtype,
+                                          grad_dtype, workspace, workspace_bytes, stream)):
+        return
+    st = _strides(strides, 3)
+    _check(lib.mics_layer_norm_backward(_matrix(dx, st, 0), _dev_ptr(dweight), _dev_ptr(dbias), _matrix(dy, st, 1), _matrix(x, st, 2),
+                                        _dev_ptr(mean), _dev_ptr(rstd), _dev_ptr(weight), rows, cols, st, dtype, param_dtype,
+                                        grad_dtype, _dev_ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def mics_dropout_add_layer_norm(y, sum, mean, rstd, x, bias, residual, weight, norm_bias, rows: int, cols: int, *, drop: float,
+                                seed: int, offset: int, eps: float, dtype: int, param_dtype: int, strides=None,
+                                stream=None) -> None:
+    """sum = residual + D(x + bias) and its layer norm in one pass; strides: y, sum, x, residual."""
+    if _done(_marshal.dropout_add_layer_norm(y, sum, mean, rstd, x, bias, residual, weight, norm_bias, rows, cols, strides, drop, seed,
+                                             offset, eps, dtype, param_dtype, stream)):
+        return
+    st = _strides(strides, 4)
+    _check(lib.mics_dropout_add_layer_norm(
+        _matrix(y, st, 0), _matrix(sum, st, 1), _dev_ptr(mean), _dev_ptr(rstd), _matrix(x, st, 2), _dev_ptr(bias),
+        _matrix(residual, st, 3), _dev_ptr(weight), _dev_ptr(norm_bias), rows, cols, st, drop, seed, offset, eps, dtype, param_dtype,
+        _stream(stream)))
+
+
+def mics_dropout_add_layer_norm_backward(dx, dresidual, dbias, dweight, dnorm_bias, dy, dsum, sum, mean, rstd, weight, rows: int,
+                                         cols: int, *, drop: float, seed: int, offset: int, dtype: int, param_dtype: int,
+                                         grad_dtype: int, workspace, workspace_bytes: int, strides=None, stream=None) -> None:
+    """Its gradients; strides: dx, dresidual, dy, dsum, sum."""
+    if _done(_marshal.dropout_add_layer_norm_backward(
+            dx, dresidual, dbias, dweight, dnorm_bias, dy, dsum, sum, mean, rstd, weight, rows, cols, strides, drop, seed, offset,
+            dtype, param_dtype, grad_dtype, workspace, workspace_bytes, stream)):
+        return
+    st = _strides(strides, 5)
+    _check(lib.mics_dropout_add_layer_norm_backward(
+        _matrix(dx, st, 0), _matrix(dresidual, st, 1), _dev_ptr(dbias), _dev_ptr(dweight), _dev_ptr(dnorm_bias), _matrix(dy, st, 2),
+        _matrix(dsum, st, 3), _matrix(sum, st, 4), _dev_ptr(mean), _dev_ptr(rstd), _dev_ptr(weight), rows, cols, st, drop, seed,
+        offset, dtype, param_dtype, grad_dtype, _dev_ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def mics_token_logprobs(logprob, entropy, lse, top_ids, top_logprobs, logits, targets, rows: int, vocab: int, *, dtype: int,
+                        top_k: int = 0, stride: Optional[int] = None, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    """Log probability of each row's target, entropy, log-sum-exp and the top_k best; stride: of the rows of logits."""
+    if stride is None:
+        stride = vocab
+    if _done(_marshal.token_logprobs(logprob, entropy, lse, top_ids, top_logprobs, logits, targets, rows, vocab, stride, top_k, dtype,
+                                     workspace, workspace_bytes, stream)):
+        return
+    _check(lib.mics_token_logprobs(_dev_ptr(logprob), _dev_ptr(entropy), _dev_ptr(lse), _dev_ptr(top_ids), _dev_ptr(top_logprobs),
+                                   _matrix(logits, (stride,)), _dev_ptr(targets), rows, vocab, stride, top_k, dtype,
+                                   _dev_ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def mics_token_logprobs_backward(dlogits, logits, targets, lse, entropy, dlogprob, dentropy, rows: int, vocab: int, *, dtype: int,
+                                 strides=None, stream=None) -> None:
+    """Gradient of the logits from those of logprob and entropy; strides: dlogits, logits."""
+    if _done(_marshal.token_logprobs_backward(dlogits, logits, targets, lse, entropy, dlogprob, dentropy, rows, vocab, strides, dtype,
+                                              stream)):
+        return
+    st = _strides(strides, 2)
+    _check(lib.mics_token_logprobs_backward(_matrix(dlogits, st, 0), _matrix(logits, st, 1), _dev_ptr(targets), _dev_ptr(lse),
+                                            _dev_ptr(entropy), _dev_ptr(dlogprob), _dev_ptr(dentropy), rows, vocab, st, dtype,
+                                            _stream(stream)))

@@ -4,6 +4,7 @@
 #include "../../include/mics.h"
 #include "../../include/mics_tuning.h"
 #include "internal.h"
+#include "layer_internal.h"
 
 #include <algorithm>
 #include <cmath>
@@ -17,7 +18,9 @@ namespace {
 
 thread_local char g_error[512] = "";
 
-int fail(int code, const char* fmt, ...)
+}  // namespace
+
+int mics::fail(int code, const char* fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -25,6 +28,10 @@ int fail(int code, const char* fmt, ...)
     va_end(ap);
     return code;
 }
+
+namespace {
+
+using mics::fail;
 
 inline uintptr_t addr(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 inline bool aligned(const void* p, size_t a) { return (addr(p) & (a - 1)) == 0; }
@@ -81,7 +88,7 @@ mics::AdamScalars adam_scalars(float lr, float beta1, float beta2, float eps, fl
 
 extern "C" {
 
-int mics_version(void) { return 300; }   // 0.3.0
+int mics_version(void) { return 400; }   // 0.4.0
 
 const char* mics_last_error(void) { return g_error; }
 

@@ -8,7 +8,7 @@
 // buffers, 8 MB 5.7 / 4.9, of 76 segments 8.0 / 6.1, Adam 5.9 / 5.1; the launch itself is 2.5 to 4 of them.
 // Whatever they do not know they leave alone and return None; the entry point then goes through ctypes.
 //
-// No state but what bind() and bind_segment() set at import.  Everything is called with the GIL held, which is given up
+// No state but what bind(), bind_layer() and bind_segment() set at import.  Everything is called with the GIL held, which is given up
 // while the library works; nothing outlives the call.
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -187,6 +187,18 @@ struct {
     decltype(&mics_replica_average_adam_shard_typed) replica_average_adam_shard_typed;
 } lib;
 constexpr Py_ssize_t kEntries = sizeof lib / sizeof(void*);
+// The entry points that bind_layer() sets.
+struct {
+    decltype(&mics_bias_dropout_add) bias_dropout_add;
+    decltype(&mics_bias_dropout_add_backward) bias_dropout_add_backward;
+    decltype(&mics_layer_norm) layer_norm;
+    decltype(&mics_layer_norm_backward) layer_norm_backward;
+    decltype(&mics_dropout_add_layer_norm) dropout_add_layer_norm;
+    decltype(&mics_dropout_add_layer_norm_backward) dropout_add_layer_norm_backward;
+    decltype(&mics_token_logprobs) token_logprobs;
+    decltype(&mics_token_logprobs_backward) token_logprobs_backward;
+} layer;
+constexpr Py_ssize_t kLayerEntries = sizeof layer / sizeof(void*);
 PyObject *device_of_thread, *raw_stream, *segment_type;
 PyObject *stream_attr, *item_attr;                 // "cuda_stream", "_type_"
 
@@ -210,6 +222,22 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
     Py_INCREF(args[2]);
     Py_XSETREF(device_of_thread, args[1]);
     Py_XSETREF(raw_stream, args[2]);
+    Py_RETURN_NONE;
+}
+
+// bind_layer(addresses in the order above)
+PyObject* bind_layer(PyObject*, PyObject* entries)
+{
+    if (!PyTuple_CheckExact(entries) || PyTuple_GET_SIZE(entries) != kLayerEntries) {
+        PyErr_SetString(PyExc_TypeError, "expected a tuple of addresses");
+        return nullptr;
+    }
+    void* at[kLayerEntries];
+    for (Py_ssize_t i = 0; i < kLayerEntries; ++i) {
+        at[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(entries, i));
+        if (!at[i] && PyErr_Occurred()) return nullptr;
+    }
+    std::memcpy((void*)&layer, at, sizeof at);
     Py_RETURN_NONE;
 }
 
@@ -256,6 +284,33 @@ class Call {
         entries = (int)PySequence_Fast_GET_SIZE(a[i]);
         for (int q = 0; plain && q < entries; ++q) pointers[q] = address(PySequence_Fast_GET_ITEM(a[i], q));
         return (const T* const*)pointers;
+    }
+    // Row strides of n matrices; None: all are packed.  Before the matrices.
+    const size_t* strides(int i, int n)
+    {
+        if (!plain || a[i] == Py_None) return nullptr;
+        plain = PySequence_Fast_GET_SIZE(a[i]) == n;
+        for (int k = 0; plain && k < n; ++k) {
+            PyObject* const v = PySequence_Fast_GET_ITEM(a[i], k);
+            plain = PyLong_CheckExact(v);
+            if (plain) row_strides[k] = PyLong_AsUnsignedLongLongMask(v);
+        }
+        return plain ? row_strides : nullptr;
+    }
+    // A matrix: what ptr() takes, or a tensor of two dimensions whose rows are `stride` elements apart.
+    void* matrix(int i, const size_t* stride)
+    {
+        if (!plain) return nullptr;
+        if (stride && THPVariable_CheckExact(a[i])) {
+            try {
+                const at::Tensor& t = THPVariable_Unpack(a[i]);
+                if (t.dim() == 2 && t.stride(1) == 1 && t.stride(0) == (int64_t)*stride) return t.data_ptr();
+            } catch (...) {
+                plain = false;
+                return nullptr;
+            }
+        }
+        return address(a[i]);
     }
     const mics_segment* segments(int i)
     {
@@ -328,10 +383,11 @@ class Call {
     int entries = 0, n_segments = 0;
 
   private:
-    static constexpr int kMaxSegments = 128;
+    static constexpr int kMaxSegments = 128, kMaxMatrices = 5;
     PyObject* const* a;
     bool plain, raised = false;
     void* pointers[MICS_MAX_GROUP];
+    size_t row_strides[kMaxMatrices];
     mics_segment segs[kMaxSegments];
 
     static bool sequence(PyObject* x) { return PyList_CheckExact(x) || PyTuple_CheckExact(x); }
@@ -351,12 +407,13 @@ class Call {
         PyObject* const names = Py_TYPE(x)->tp_dict;       // of a ctypes array's type: _type_ is its items' type
         return names && segment_type && PyDict_GetItem(names, item_attr) == segment_type;
     }
-    // p pointer, t table of them, g segments, i integer, b flag, f number, s stream
+    // p pointer, t table of them, z row strides, g segments, i integer, b flag, f number, s stream
     static bool of_kind(PyObject* x, char kind)
     {
         switch (kind) {
             case 'p': return x == Py_None || PyLong_CheckExact(x) || THPVariable_CheckExact(x);
             case 't': return sequence(x) && PySequence_Fast_GET_SIZE(x) <= MICS_MAX_GROUP;
+            case 'z': return x == Py_None || sequence(x);
             case 'g': return segment_list(x);
             case 'i': return PyLong_CheckExact(x);
             case 'b': return PyBool_Check(x) || PyLong_CheckExact(x);
@@ -536,6 +593,163 @@ MICS_CALL(update_typed)
     });
 }
 
+// Stride k of a table that may not be there.
+const size_t* at(const size_t* strides, int k) { return strides ? strides + k : nullptr; }
+
+struct Drop {
+    float drop;
+    uint64_t seed, offset;
+    Drop(Call& c, int i) : drop(c.real(i)), seed(c.size(i + 1)), offset(c.size(i + 2)) {}
+};
+
+// out x bias residual rows cols strides drop seed offset dtype param_dtype stream
+MICS_CALL(bias_dropout_add)
+{
+    Call c(args, n, "ppppiizfiiiis");
+    const size_t* const st = c.strides(6, 3);
+    void* const out = c.matrix(0, at(st, 0));
+    const void *const x = c.matrix(1, at(st, 1)), *const bias = c.ptr(2), *const residual = c.matrix(3, at(st, 2));
+    const size_t rows = c.size(4), cols = c.size(5);
+    const Drop d(c, 7);
+    const int dtype = c.num(10), param = c.num(11);
+    void* const s = c.stream(12);
+    return c.run([&] { return layer.bias_dropout_add(out, x, bias, residual, rows, cols, st, d.drop, d.seed, d.offset, dtype, param, s); });
+}
+
+// dx dbias dout rows cols strides drop seed offset dtype grad_dtype workspace workspace_bytes stream
+MICS_CALL(bias_dropout_add_backward)
+{
+    Call c(args, n, "pppiizfiiiipis");
+    const size_t* const st = c.strides(5, 2);
+    void *const dx = c.matrix(0, at(st, 0)), *const dbias = c.ptr(1);
+    const void* const dout = c.matrix(2, at(st, 1));
+    const size_t rows = c.size(3), cols = c.size(4);
+    const Drop d(c, 6);
+    const int dtype = c.num(9), grad = c.num(10);
+    void* const work = c.ptr(11);
+    const size_t bytes = c.size(12);
+    void* const s = c.stream(13);
+    return c.run([&] {
+        return layer.bias_dropout_add_backward(dx, dbias, dout, rows, cols, st, d.drop, d.seed, d.offset, dtype, grad, work, bytes, s);
+    });
+}
+
+// y mean rstd x weight bias rows cols strides eps dtype param_dtype stream
+MICS_CALL(layer_norm)
+{
+    Call c(args, n, "ppppppiizfiis");
+    const size_t* const st = c.strides(8, 2);
+    void* const y = c.matrix(0, at(st, 0));
+    float *const mean = (float*)c.ptr(1), *const rstd = (float*)c.ptr(2);
+    const void *const x = c.matrix(3, at(st, 1)), *const weight = c.ptr(4), *const bias = c.ptr(5);
+    const size_t rows = c.size(6), cols = c.size(7);
+    const float eps = c.real(9);
+    const int dtype = c.num(10), param = c.num(11);
+    void* const s = c.stream(12);
+    return c.run([&] { return layer.layer_norm(y, mean, rstd, x, weight, bias, rows, cols, st, eps, dtype, param, s); });
+}
+
+// dx dweight dbias dy x mean rstd weight rows cols strides dtype param_dtype grad_dtype workspace workspace_bytes stream
+MICS_CALL(layer_norm_backward)
+{
+    Call c(args, n, "ppppppppiiziiipis");
+    const size_t* const st = c.strides(10, 3);
+    void *const dx = c.matrix(0, at(st, 0)), *const dweight = c.ptr(1), *const dbias = c.ptr(2);
+    const void *const dy = c.matrix(3, at(st, 1)), *const x = c.matrix(4, at(st, 2));
+    const float *const mean = (float*)c.ptr(5), *const rstd = (float*)c.ptr(6);
+    const void* const weight = c.ptr(7);
+    const size_t rows = c.size(8), cols = c.size(9);
+    const int dtype = c.num(11), param = c.num(12), grad = c.num(13);
+    void* const work = c.ptr(14);
+    const size_t bytes = c.size(15);
+    void* const s = c.stream(16);
+    return c.run([&] {
+        return layer.layer_norm_backward(dx, dweight, dbias, dy, x, mean, rstd, weight, rows, cols, st, dtype, param, grad, work,
+                                         bytes, s);
+    });
+}
+
+// y sum mean rstd x bias residual weight norm_bias rows cols strides drop seed offset eps dtype param_dtype stream
+MICS_CALL(dropout_add_layer_norm)
+{
+    Call c(args, n, "pppppppppiizfiifiis");
+    const size_t* const st = c.strides(11, 4);
+    void *const y = c.matrix(0, at(st, 0)), *const sum = c.matrix(1, at(st, 1));
+    float *const mean = (float*)c.ptr(2), *const rstd = (float*)c.ptr(3);
+    const void *const x = c.matrix(4, at(st, 2)), *const bias = c.ptr(5), *const residual = c.matrix(6, at(st, 3));
+    const void *const weight = c.ptr(7), *const norm_bias = c.ptr(8);
+    const size_t rows = c.size(9), cols = c.size(10);
+    const Drop d(c, 12);
+    const float eps = c.real(15);
+    const int dtype = c.num(16), param = c.num(17);
+    void* const s = c.stream(18);
+    return c.run([&] {
+        return layer.dropout_add_layer_norm(y, sum, mean, rstd, x, bias, residual, weight, norm_bias, rows, cols, st, d.drop, d.seed,
+                                            d.offset, eps, dtype, param, s);
+    });
+}
+
+// dx dresidual dbias dweight dnorm_bias dy dsum sum mean rstd weight rows cols strides drop seed offset dtype param_dtype
+// grad_dtype workspace workspace_bytes stream
+MICS_CALL(dropout_add_layer_norm_backward)
+{
+    Call c(args, n, "pppppppppppiizfiiiiipis");
+    const size_t* const st = c.strides(13, 5);
+    void *const dx = c.matrix(0, at(st, 0)), *const dresidual = c.matrix(1, at(st, 1));
+    void *const dbias = c.ptr(2), *const dweight = c.ptr(3), *const dnorm_bias = c.ptr(4);
+    const void *const dy = c.matrix(5, at(st, 2)), *const dsum = c.matrix(6, at(st, 3)), *const sum = c.matrix(7, at(st, 4));
+    const float *const mean = (float*)c.ptr(8), *const rstd = (float*)c.ptr(9);
+    const void* const weight = c.ptr(10);
+    const size_t rows = c.size(11), cols = c.size(12);
+    const Drop d(c, 14);
+    const int dtype = c.num(17), param = c.num(18), grad = c.num(19);
+    void* const work = c.ptr(20);
+    const size_t bytes = c.size(21);
+    void* const s = c.stream(22);
+    return c.run([&] {
+        return layer.dropout_add_layer_norm_backward(dx, dresidual, dbias, dweight, dnorm_bias, dy, dsum, sum, mean, rstd, weight,
+                                                     rows, cols, st, d.drop, d.seed, d.offset, dtype, param, grad, work, bytes, s);
+    });
+}
+
+// logprob entropy lse top_ids top_logprobs logits targets rows vocab stride top_k dtype workspace workspace_bytes stream
+MICS_CALL(token_logprobs)
+{
+    Call c(args, n, "pppppppiiiiipis");
+    const size_t stride = c.size(9);
+    float *const logprob = (float*)c.ptr(0), *const entropy = (float*)c.ptr(1), *const lse = (float*)c.ptr(2);
+    int64_t* const ids = (int64_t*)c.ptr(3);
+    float* const top = (float*)c.ptr(4);
+    const void* const logits = c.matrix(5, &stride);
+    const int64_t* const targets = (const int64_t*)c.ptr(6);
+    const size_t rows = c.size(7), vocab = c.size(8);
+    const int k = c.num(10), dtype = c.num(11);
+    void* const work = c.ptr(12);
+    const size_t bytes = c.size(13);
+    void* const s = c.stream(14);
+    return c.run([&] {
+        return layer.token_logprobs(logprob, entropy, lse, ids, top, logits, targets, rows, vocab, stride, k, dtype, work, bytes, s);
+    });
+}
+
+// dlogits logits targets lse entropy dlogprob dentropy rows vocab strides dtype stream
+MICS_CALL(token_logprobs_backward)
+{
+    Call c(args, n, "pppppppiizis");
+    const size_t* const st = c.strides(9, 2);
+    void* const dlogits = c.matrix(0, at(st, 0));
+    const void* const logits = c.matrix(1, at(st, 1));
+    const int64_t* const targets = (const int64_t*)c.ptr(2);
+    const float *const lse = (float*)c.ptr(3), *const entropy = (float*)c.ptr(4), *const dlogprob = (float*)c.ptr(5);
+    const float* const dentropy = (float*)c.ptr(6);
+    const size_t rows = c.size(7), vocab = c.size(8);
+    const int dtype = c.num(10);
+    void* const s = c.stream(11);
+    return c.run([&] {
+        return layer.token_logprobs_backward(dlogits, logits, targets, lse, entropy, dlogprob, dentropy, rows, vocab, st, dtype, s);
+    });
+}
+
 #define MICS_METHOD(name) {#name, (PyCFunction)(void (*)())name, METH_FASTCALL, "A whole call; None if an argument is not plain."}
 
 PyMethodDef methods[] = {
@@ -547,6 +761,10 @@ PyMethodDef methods[] = {
     MICS_METHOD(gather), MICS_METHOD(gather_coalesced), MICS_METHOD(reduce), MICS_METHOD(reduce_typed),
     MICS_METHOD(reduce_coalesced), MICS_METHOD(reduce_coalesced_typed), MICS_METHOD(average), MICS_METHOD(adam),
     MICS_METHOD(adam_typed), MICS_METHOD(update), MICS_METHOD(update_typed),
+    {"bind_layer", bind_layer, METH_O, "Sets the entry points of the operators between gather and reduction."},
+    MICS_METHOD(bias_dropout_add), MICS_METHOD(bias_dropout_add_backward), MICS_METHOD(layer_norm),
+    MICS_METHOD(layer_norm_backward), MICS_METHOD(dropout_add_layer_norm), MICS_METHOD(dropout_add_layer_norm_backward),
+    MICS_METHOD(token_logprobs), MICS_METHOD(token_logprobs_backward),
     {nullptr, nullptr, 0, nullptr},
 };
 
