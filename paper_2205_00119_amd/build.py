@@ -6,7 +6,7 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libmics.so")
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("api.cpp", "layer_api.cpp", "kernels.hip", "layer.hip", "logprobs.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("api.cpp", "layer_api.cpp", "kernels.hip", "norm.hip", "dropout.hip", "logprobs.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

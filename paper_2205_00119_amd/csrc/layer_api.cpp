@@ -336,7 +336,7 @@ int mics_bias_dropout_add_backward(void* dx, void* dbias, const void* dout, size
 size_t mics_token_logprobs_workspace_bytes(size_t rows, size_t vocab, int top_k)
 {
     if (!column_sizes(rows, vocab) || top_k < 0 || top_k > MICS_MAX_TOP) return 0;
-    const int splits = mics::row_splits(rows, vocab);
+    const int splits = mics::row_splits(rows, vocab, top_k);
     return splits > 1 ? rows * (size_t)splits * mics::split_bytes(top_k) : 0;
 }
 

@@ -1,4 +1,4 @@
-// Between the argument checks (layer_api.cpp) and the launchers (layer.hip, logprobs.hip) of the operators that a
+// Between the argument checks (layer_api.cpp) and the launchers (norm.hip, dropout.hip, logprobs.hip) of the operators that a
 // transformer layer's training step runs between the parameter gather and the gradient reduction.
 #pragma once
 
@@ -30,7 +30,7 @@ struct ConstRows {
 
 // Kinds: 0 bf16, 1 IEEE binary16, 2 binary32.  `kind` is that of the matrices, `param` that of the vectors.
 struct NormForward {
-    Rows y, sum;                          // sum: with `residual` or dropout only
+    Rows y, sum;                          // sum may be NULL
     float *mean, *rstd;                   // may be NULL
     ConstRows x, residual;
     const void *bias, *weight, *norm_bias;   // may be NULL
@@ -63,10 +63,10 @@ struct DropoutPass {
     float* parts;                         // backward with dbias
 };
 
-// Column sums are formed in at most so many groups of rows.
-constexpr size_t kMostParts = 512;
+// Column sums are formed in groups of rows: of three sums at most so many groups, of one twice as many.
+constexpr size_t kMostParts = 256;
 // Rows of more elements than this do not stay in a workgroup's registers in the backward pass.
-constexpr size_t kTiledCols = 16384;
+constexpr size_t kTiledCols = 8192;
 constexpr size_t row_sums_floats(size_t rows, size_t cols) { return cols > kTiledCols ? 2 * rows : 0; }
 constexpr size_t parts_floats(size_t rows, size_t cols) { return (rows < kMostParts ? rows : kMostParts) * 3 * cols; }
 constexpr size_t kMostCols = size_t{1} << 24;
@@ -100,7 +100,7 @@ struct LogProbsBackward {
 };
 constexpr int kMostTop = 64;
 // Workgroups that share a row, and the bytes that one of them leaves for the join.
-int row_splits(size_t rows, size_t vocab);
+int row_splits(size_t rows, size_t vocab, int top);
 constexpr size_t split_bytes(int top) { return 16 + 8 * (size_t)top; }
 int launch_logprobs(const LogProbs& a, int kind, void* stream);
 int launch_logprobs_backward(const LogProbsBackward& a, int kind, void* stream);

@@ -21,15 +21,16 @@ constexpr float kFar = -200.f;
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
 __device__ __forceinline__ float infinity() { return __builtin_inff(); }
 
-// m: the largest logit (NaN aside), -inf if there is none.  A NaN or +inf among the logits makes z and t NaN.
+// z = sum e^(x-base), t = sum (x-base) e^(x-base).  A NaN or +inf among the logits makes z NaN; logits of -inf alone, or
+// none, leave z = 0.
 struct Stat {
-    float m, z, t;
-    __device__ __forceinline__ float base() const { return fmaxf(m, kLowest); }
-    __device__ __forceinline__ void move_to(float base_to)
+    float base, z, t;
+    __device__ __forceinline__ void move_to(float to)
     {
-        const float d = base() - base_to, e = exp_of(d);
+        const float d = base - to, e = exp_of(d);
         t = e * __builtin_fmaf(fmaxf(d, kFar), z, t);
         z *= e;
+        base = to;
     }
 };
 
@@ -52,8 +53,8 @@ __device__ __forceinline__ float wave_max(float v)
 // Largest of each aligned run of LANES lanes, in all of them.
 template <int LANES> __device__ __forceinline__ float run_max(float v)
 {
-    v = dpp_max<0xB1, 0xF>(v);                                  // quad_perm 1,0,3,2
-    v = dpp_max<0x4E, 0xF>(v);                                  // quad_perm 2,3,0,1
+    if constexpr (LANES >= 2) v = dpp_max<0xB1, 0xF>(v);        // quad_perm 1,0,3,2
+    if constexpr (LANES >= 4) v = dpp_max<0x4E, 0xF>(v);        // quad_perm 2,3,0,1
     if constexpr (LANES >= 8) v = dpp_max<0x141, 0xF>(v);       // row_half_mirror
     if constexpr (LANES >= 16) v = dpp_max<0x140, 0xF>(v);      // row_mirror
     return v;
@@ -82,8 +83,8 @@ template <int LANES, bool TOP> struct LogProbsLds {
     Stat stat[LANES / 64];
 };
 template <int LANES> struct LogProbsLds<LANES, true> {
-    Stat stat[LANES / 64];
     float run[64];
+    Stat stat[LANES / 64];
     float threshold;
     int count;
     Key best[kMostTop];
@@ -113,71 +114,40 @@ template <int KIND> struct Span {
     }
 };
 
-template <int N> __device__ __forceinline__ void add_logits(Stat& s, const float (&x)[N])
+// How far a logit may be above a lane's base before its sums are moved to a new one: e^8 costs no precision.
+constexpr float kSlack = 8.f;
+
+template <int N> __device__ __forceinline__ float largest(const float (&x)[N])
 {
-    float most = s.m;
+    float most = -infinity();
     #pragma unroll
     for (int i = 0; i < N; ++i) most = fmaxf(most, x[i]);
-    const float base = fmaxf(most, kLowest);
-    s.move_to(base);
-    s.m = most;
+    return most;
+}
+template <bool ENTROPY, int N> __device__ __forceinline__ void add_logits(Stat& s, const float (&x)[N], float most)
+{
+    if (__builtin_amdgcn_ballot_w64(most > s.base + kSlack)) s.move_to(fmaxf(most, s.base));
     #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float d = x[i] - base, e = exp_of(d);
+        const float d = x[i] - s.base, e = exp_of(d);
         s.z += e;
-        s.t = __builtin_fmaf(fmaxf(d, kFar), e, s.t);
+        if constexpr (ENTROPY) s.t = __builtin_fmaf(fmaxf(d, kFar), e, s.t);
     }
 }
 
-// A lane's part of the span: U vectors in flight.
-template <int KIND, int LANES, int U> __device__ __forceinline__ Stat lane_stat(const Span<KIND>& span)
+// Joins the lanes of a wavefront, in a fixed order; the result is in every lane.
+__device__ __forceinline__ Stat wave_stat(Stat s)
 {
-    Stat s = {-infinity(), 0.f, 0.f};
-    const unsigned whole = span.whole();
-    for (unsigned c = span.begin + threadIdx.x; c < whole; c += LANES * U) {
-        Raw<KIND> r[U];
-        #pragma unroll
-        for (int u = 0; u < U; ++u) r[u] = load_vec<KIND>(span.row + (size_t)min(c + u * LANES, whole - 1) * (kVec * kWidth<KIND>), kVec);
-        #pragma unroll
-        for (int u = 0; u < U; u += 2) {
-            float x[2][kVec], both[2 * kVec];
-            #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                unpack<KIND>(r[u + h], x[h]);
-                const bool in = c + (u + h) * LANES < whole;
-                #pragma unroll
-                for (int i = 0; i < kVec; ++i) both[h * kVec + i] = in ? x[h][i] : -infinity();
-            }
-            add_logits(s, both);
-        }
-    }
-    if (whole >= span.begin && whole < span.end && threadIdx.x == 0) {
-        float x[kVec];
-        span.vec(whole, x);
-        add_logits(s, x);
-    }
-    return s;
+    s.move_to(wave_max(s.base));
+    return {s.base, wave_sum(s.z), wave_sum(s.t)};
 }
-
-// The workgroup's, in lane order within wavefronts, then by wavefront; in all lanes.
 template <int LANES> __device__ __forceinline__ Stat block_stat(Stat (&lds)[LANES / 64], Stat s)
 {
-    const float most = wave_max(s.m);
-    s.move_to(fmaxf(most, kLowest));
-    s = {most, wave_sum(s.z), wave_sum(s.t)};
-    const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63u) == 0) lds[wave] = s;
-    __syncthreads();
-    Stat all = lds[0];
-    for (int w = 1; w < LANES / 64; ++w) all.m = fmaxf(all.m, lds[w].m);
-    float z = 0.f, t = 0.f;
-    for (int w = 0; w < LANES / 64; ++w) {
-        Stat part = lds[w];
-        part.move_to(all.base());
-        z += part.z;
-        t += part.t;
-    }
-    return {all.m, z, t};
+    s = wave_stat(s);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (lane == 0) lds[wave] = s;
+    barrier_lds();
+    return wave_stat(lane < LANES / 64 ? lds[lane] : Stat{kLowest, 0.f, 0.f});
 }
 
 // Calls f(x, index) for every element of the span, each by one lane.
@@ -200,83 +170,121 @@ template <int LANES> __device__ __forceinline__ void keep_candidate(LogProbsLds<
     if (at < kCandidates) lds.candidate[at] = key_of(x, index);
 }
 
-// The `top` best of the span into lds.best in order, behind a barrier; 0 where the span has fewer.  most: the lane's
-// largest logit.  The top-th largest of 64 runs' largest logits is at most the top-th largest logit, and few others
-// reach it: those that do are ranked.  Where too many do (equal logits, a mask that leaves fewer than `top`), those above
-// it, and as many of those equal to it, lowest index first; failing that, one after the other.
-template <int KIND, int LANES> __device__ __forceinline__ void best_of(LogProbsLds<LANES, true>& lds, const Span<KIND>& span, int top, float most)
+// The top-th largest of the largest logits of 64 runs of lanes: at most the top-th largest logit of all, and few others
+// reach it.  Also empties the list of candidates.
+template <int LANES> __device__ __forceinline__ float reached_by(LogProbsLds<LANES, true>& lds, int top, float most)
 {
     constexpr int kRun = LANES / 64;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int tid = threadIdx.x, lane = tid & 63;
     const float of_run = run_max<kRun>(most);
     if (tid % kRun == 0) lds.run[tid / kRun] = of_run;
-    if (tid < kMostTop) lds.best[tid] = 0;
     if (tid == 0) lds.count = 0;
-    __syncthreads();
-    if (wave == 0) {
+    barrier_lds();
+    if (tid < 64) {
         const float mine = lds.run[lane];
         int rank = 0;
         for (int j = 0; j < 64; ++j) {
-            const float other = lds.run[j];
+            const float other = lane_value(mine, j);
             rank += other > mine || (other == mine && j < lane);
         }
         if (rank == top - 1) lds.threshold = mine;
     }
-    __syncthreads();
-    const float threshold = lds.threshold;
+    barrier_lds();
+    return lds.threshold;
+}
+
+// The first `top` of the n candidates in order into lds.best, n the same in all lanes.  Many candidates are thinned out
+// first, by the threshold of their own runs (300 x 100000 bf16, half of them masked, 50 alternatives, with 256 lanes a row: some
+// 1200 candidates, 584 us without, 64 so).
+template <int LANES> __device__ __forceinline__ void rank_candidates(LogProbsLds<LANES, true>& lds, int n, int top)
+{
+    if (n > 3 * 64) {
+        constexpr int kEach = kCandidates / LANES;
+        Key mine[kEach];
+        float most = -infinity();
+        #pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int i = threadIdx.x + j * LANES;
+            mine[j] = i < n ? lds.candidate[i] : 0;
+            if (mine[j]) most = fmaxf(most, value_of(mine[j]));
+        }
+        const float threshold = reached_by<LANES>(lds, top, most);
+        #pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (mine[j] && !(value_of(mine[j]) < threshold)) lds.candidate[atomicAdd(&lds.count, 1)] = mine[j];
+        barrier_lds();
+        n = lds.count;
+    }
+    for (int i = threadIdx.x; i < n; i += LANES) {
+        const Key mine = lds.candidate[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += lds.candidate[j] > mine;
+        if (rank < top) lds.best[rank] = mine;
+    }
+}
+
+// Fills lds.best from place `have` on with the first elements of the span that equal `value`.  By one wavefront.
+template <int KIND, int LANES>
+__device__ __forceinline__ void fill_equal(LogProbsLds<LANES, true>& lds, const Span<KIND>& span, int have, int top, float value)
+{
+    const int lane = threadIdx.x & 63;
+    for (unsigned c = span.begin; c < span.end && have < top; c += 64) {
+        float x[kVec];
+        unsigned equal = 0;
+        const int valid = c + lane < span.end ? valid_at(c + lane, span.cols) : 0;
+        if (valid > 0) {
+            span.vec(c + lane, x);
+            #pragma unroll
+            for (int i = 0; i < kVec; ++i) equal |= (unsigned)(i < valid && x[i] == value) << i;
+        }
+        // elements before this lane's: bit by bit of the lanes' counts
+        const int count = __popc(equal);
+        int before = 0, total = 0;
+        #pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const unsigned long long lanes = __ballot(count >> b & 1);
+            before += __popcll(lanes & ((1ull << lane) - 1)) << b;
+            total += __popcll(lanes) << b;
+        }
+        int at = have + before;
+        #pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (equal >> i & 1) {
+                if (at < top) lds.best[at] = key_of(value, (c + lane) * kVec + i);
+                ++at;
+            }
+        have += total;
+    }
+}
+
+// The `top` best of a span that the candidates did not settle (too many of them, NaN):
+// those that reach the threshold of the whole span; where these are too many still, those above it and as many of those
+// equal to it, lowest index first; failing that, one after the other.
+template <int KIND, int LANES> __device__ __forceinline__ void best_of_any(LogProbsLds<LANES, true>& lds, const Span<KIND>& span, int top)
+{
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    float most = -infinity();
+    each<KIND, LANES>(span, [&](float x, unsigned) { most = fmaxf(most, x); });
+    const float threshold = reached_by<LANES>(lds, top, most);
     // -inf: all elements reach it
     const bool all = threshold == -infinity();
     if (!all) {
         each<KIND, LANES>(span, [&](float x, unsigned i) { if (!(x < threshold)) keep_candidate(lds, x, i); });
-        __syncthreads();
+        barrier_lds();
     }
     bool fill = false;
     if (all || lds.count > kCandidates) {
-        __syncthreads();
+        barrier_lds();
         if (tid == 0) lds.count = 0;
-        __syncthreads();
+        barrier_lds();
         each<KIND, LANES>(span, [&](float x, unsigned i) { if (!(x <= threshold)) keep_candidate(lds, x, i); });
-        __syncthreads();
+        barrier_lds();
         fill = true;
     }
     const int n = lds.count;
     if (n <= kCandidates) {
-        for (int i = tid; i < n; i += LANES) {
-            const Key mine = lds.candidate[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += lds.candidate[j] > mine;
-            if (rank < top) lds.best[rank] = mine;
-        }
-        if (fill && wave == 0) {
-            int have = n;
-            for (unsigned c = span.begin; c < span.end && have < top; c += 64) {
-                float x[kVec];
-                unsigned equal = 0;
-                const int valid = c + lane < span.end ? valid_at(c + lane, span.cols) : 0;
-                if (valid > 0) {
-                    span.vec(c + lane, x);
-                    #pragma unroll
-                    for (int i = 0; i < kVec; ++i) equal |= (unsigned)(i < valid && x[i] == threshold) << i;
-                }
-                // elements before this lane's: bit by bit of the lanes' counts
-                const int count = __popc(equal);
-                int before = 0, total = 0;
-                #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const unsigned long long lanes = __ballot(count >> b & 1);
-                    before += __popcll(lanes & ((1ull << lane) - 1)) << b;
-                    total += __popcll(lanes) << b;
-                }
-                int at = have + before;
-                #pragma unroll
-                for (int i = 0; i < kVec; ++i)
-                    if (equal >> i & 1) {
-                        if (at < top) lds.best[at] = key_of(threshold, (c + lane) * kVec + i);
-                        ++at;
-                    }
-                have += total;
-            }
-        }
+        rank_candidates<LANES>(lds, n, top);
+        if (fill && wave == 0) fill_equal<KIND, LANES>(lds, span, n, top, threshold);
     } else {
         Key last = ~(Key)0;
         for (int k = 0; k < top; ++k) {
@@ -291,44 +299,50 @@ template <int KIND, int LANES> __device__ __forceinline__ void best_of(LogProbsL
                 if (other > next) next = other;
             }
             if (lane == 0) lds.wave_best[wave] = next;
-            __syncthreads();
+            barrier_lds();
             for (int w = 0; w < LANES / 64; ++w)
                 if (lds.wave_best[w] > next) next = lds.wave_best[w];
             if (tid == 0) lds.best[k] = next;
             last = next;
-            __syncthreads();
+            barrier_lds();
         }
     }
-    __syncthreads();
 }
 
+// A row's target and its logit, loaded before the pass over the row, which hides both.
+struct Target {
+    int64_t at;
+    float logit;
+};
+template <int KIND> __device__ __forceinline__ Target target_of(const LogProbs& a, size_t row)
+{
+    const int64_t at = a.targets[row];
+    const size_t column = at < 0 ? 0 : at >= (int64_t)a.vocab ? a.vocab - 1 : (size_t)at;
+    const char* const p = (const char*)a.logits.data + (row * a.logits.stride + column) * kWidth<KIND>;
+    return {at, KIND == kF32 ? *(const float*)p : widen<KIND>(*(const uint16_t*)p)};
+}
 // What a row's statistics give.  By one lane.
-template <int KIND> __device__ __forceinline__ float finish_row(const LogProbs& a, size_t row, const Stat& s)
+__device__ __forceinline__ void finish_row(const LogProbs& a, size_t row, const Stat& s, const Target& target)
 {
     // no logit but -inf: nothing can be drawn
     const float log_z = __builtin_logf(s.z);
-    const float lse = s.z == 0.f ? -infinity() : s.m + log_z;
-    if (a.lse) a.lse[row] = lse;
+    if (a.lse) a.lse[row] = s.z == 0.f ? -infinity() : s.base + log_z;
     if (a.entropy) a.entropy[row] = s.z == 0.f ? 0.f : log_z - s.t / s.z;
-    const int64_t target = a.targets[row];
-    float logprob = 0.f;
-    if (target >= (int64_t)a.vocab) logprob = __builtin_nanf("");
-    else if (target >= 0) {
-        const char* const at = (const char*)a.logits.data + (row * a.logits.stride + (size_t)target) * kWidth<KIND>;
-        const float x = KIND == kF32 ? *(const float*)at : widen<KIND>(*(const uint16_t*)at);
-        logprob = s.z == 0.f ? -infinity() : x - s.m - log_z;
-    }
+    float logprob = s.z == 0.f ? -infinity() : target.logit - s.base - log_z;
+    if (target.at < 0) logprob = 0.f;
+    if (target.at >= (int64_t)a.vocab) logprob = __builtin_nanf("");
     a.logprob[row] = logprob;
-    return lse;
 }
 __device__ __forceinline__ void write_best(const LogProbs& a, size_t row, int k, Key key, const Stat& s)
 {
     a.top_ids[row * a.top + k] = index_of(key);
     const float v = value_of(key);
-    a.top_logprobs[row * a.top + k] = s.z == 0.f ? -infinity() : v - s.m - __builtin_logf(s.z);
+    a.top_logprobs[row * a.top + k] = s.z == 0.f ? -infinity() : v - s.base - __builtin_logf(s.z);
 }
 
-template <int KIND, int LANES, int U, bool TOP>
+// One pass: U vectors of every lane are worked on while the next U are loaded.  TOP: the first U tell a threshold, and what
+// reaches it is kept as a candidate on the way.
+template <int KIND, int LANES, int U, bool TOP, bool ENTROPY, bool NT>
 __global__ __launch_bounds__(LANES) void logprobs_kernel(LogProbsArgs p)
 {
     const LogProbs& a = p.a;
@@ -340,11 +354,95 @@ __global__ __launch_bounds__(LANES) void logprobs_kernel(LogProbsArgs p)
         const unsigned split = (unsigned)(unit - row * p.splits);
         const Span<KIND> span = {(const char*)a.logits.data + row * a.logits.stride * kWidth<KIND>, split * p.chunk,
                                  min(vecs, (split + 1) * p.chunk), a.vocab};
-        const Stat mine = lane_stat<KIND, LANES, U>(span);
-        const Stat s = block_stat<LANES>(lds.stat, mine);
-        if constexpr (TOP) best_of<KIND, LANES>(lds, span, a.top, mine.m);
+        const unsigned whole = span.whole();
+        const Target target = target_of<KIND>(a, row);
+        Stat s = {kLowest, 0.f, 0.f};
+        float threshold = -infinity();
+        bool masked = true;                  // the first vectors hold too few logits but -inf: all but those are candidates
+        auto load = [&](Raw<KIND> (&r)[U], unsigned from) {
+            #pragma unroll
+            for (int u = 0; u < U; ++u)
+                r[u] = load_vec<KIND, NT>(span.row + (size_t)min(from + u * LANES, whole - 1) * (kVec * kWidth<KIND>), kVec);
+        };
+        auto keep = [&](const float* x, unsigned c) {
+            if constexpr (TOP) {
+                #pragma unroll
+                for (int i = 0; i < kVec; ++i)
+                    if (!(x[i] < threshold)) keep_candidate(lds, x[i], c * kVec + i);
+            }
+        };
+        auto read = [&](auto PART, const Raw<KIND> (&r)[U], unsigned c, float (&x)[U * kVec]) {
+            #pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float v[kVec];
+                unpack<KIND>(r[u], v);
+                const bool in = !decltype(PART)::value || c + u * LANES < whole;
+                #pragma unroll
+                for (int i = 0; i < kVec; ++i) x[u * kVec + i] = in ? v[i] : -infinity();
+            }
+        };
+        auto add = [&](const float (&x)[U * kVec], float most, unsigned c) {
+            if (TOP && !(most < threshold)) {
+                #pragma unroll
+                for (int u = 0; u < U; ++u) keep(x + u * kVec, c + u * LANES);
+            }
+            add_logits<ENTROPY>(s, x, most);
+        };
+        if constexpr (TOP)
+            if (threadIdx.x < kMostTop) lds.best[threadIdx.x] = 0;
+        if (span.begin < whole) {
+            constexpr unsigned kStep = LANES * U;
+            Raw<KIND> r[2][U];
+            unsigned at = span.begin + threadIdx.x;                  // the first lane's is below `whole`
+            load(r[0], at);
+            load(r[1], at + kStep);
+            {
+                float x[U * kVec];
+                read(std::true_type{}, r[0], at, x);
+                const float most = largest(x);
+                if constexpr (TOP) {
+                    threshold = reached_by<LANES>(lds, a.top, most);
+                    masked = threshold == -infinity();
+                    threshold = fmaxf(threshold, kLowest);
+                }
+                add(x, most, at);
+            }
+            for (unsigned from = span.begin + kStep; from < whole;) {
+                #pragma unroll
+                for (int k = 1; k >= 0; --k) {
+                    if (from >= whole) break;
+                    at = from + threadIdx.x;
+                    load(r[1 - k], at + kStep);
+                    float x[U * kVec];
+                    if (from + kStep <= whole) read(std::false_type{}, r[k], at, x);
+                    else read(std::true_type{}, r[k], at, x);
+                    add(x, largest(x), at);
+                    from += kStep;
+                }
+            }
+        } else if constexpr (TOP) {
+            threshold = fmaxf(reached_by<LANES>(lds, a.top, -infinity()), kLowest);
+        }
+        if (whole >= span.begin && whole < span.end && threadIdx.x == 0) {       // the last part of a vector
+            float x[kVec];
+            span.vec(whole, x);
+            add_logits<ENTROPY>(s, x, largest(x));
+            keep(x, whole);
+        }
+        s = block_stat<LANES>(lds.stat, s);
+        if constexpr (TOP) {
+            const int n = lds.count;      // behind block_stat's barrier
+            barrier_lds();              // and before it is set back
+            if (s.z == s.z && n <= kCandidates) {
+                rank_candidates<LANES>(lds, n, a.top);
+                if (masked && n < a.top && threadIdx.x < 64) fill_equal<KIND, LANES>(lds, span, n, a.top, -infinity());
+            } else {
+                best_of_any<KIND, LANES>(lds, span, a.top);
+            }
+            barrier_lds();
+        }
         if (p.splits == 1) {
-            if (threadIdx.x == 0) finish_row<KIND>(a, row, s);
+            if (threadIdx.x == 0) finish_row(a, row, s, target);
             if constexpr (TOP)
                 if ((int)threadIdx.x < a.top) write_best(a, row, threadIdx.x, lds.best[threadIdx.x], s);
         } else {
@@ -353,50 +451,34 @@ __global__ __launch_bounds__(LANES) void logprobs_kernel(LogProbsArgs p)
             if constexpr (TOP)
                 if ((int)threadIdx.x < a.top) ((Key*)(part + 16))[threadIdx.x] = lds.best[threadIdx.x];
         }
-        __syncthreads();       // the LDS is free for the next row
+        barrier_lds();       // the LDS is free for the next row
     }
 }
 
-// Joins the splits of a row, one workgroup a row.  A key's rank is its place in its own list and what every other list
-// has above it.
+// Joins the splits of a row, one workgroup a row: at most 64 of them, with at most kCandidates keys.
 constexpr int kJoinLanes = 256;
-template <int KIND>
+template <int KIND, bool TOP>
 __global__ __launch_bounds__(kJoinLanes) void join_kernel(LogProbsArgs p)
 {
     const LogProbs& a = p.a;
-    extern __shared__ Key lists[];
+    __shared__ LogProbsLds<kJoinLanes, TOP> lds;
     const size_t bytes = split_bytes(a.top);
+    const int lane = threadIdx.x & 63;
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const char* const parts = (const char*)a.parts + row * p.splits * bytes;
-        Stat s = {-infinity(), 0.f, 0.f};
-        for (int i = 0; i < p.splits; ++i) s.m = fmaxf(s.m, ((const Stat*)(parts + i * bytes))->m);
-        for (int i = 0; i < p.splits; ++i) {
-            Stat part = *(const Stat*)(parts + i * bytes);
-            part.move_to(s.base());
-            s.z += part.z;
-            s.t += part.t;
+        const Target target = target_of<KIND>(a, row);
+        const Stat s = wave_stat(lane < p.splits ? *(const Stat*)(parts + lane * bytes) : Stat{kLowest, 0.f, 0.f});
+        if (threadIdx.x == 0) finish_row(a, row, s, target);
+        if constexpr (TOP) {
+            const int n = p.splits * a.top;
+            for (int i = threadIdx.x; i < n; i += kJoinLanes)
+                lds.candidate[i] = ((const Key*)(parts + (i / a.top) * bytes + 16))[i % a.top];
+            barrier_lds();
+            rank_candidates<kJoinLanes>(lds, n, a.top);
+            barrier_lds();
+            if ((int)threadIdx.x < a.top) write_best(a, row, threadIdx.x, lds.best[threadIdx.x], s);
+            barrier_lds();
         }
-        if (threadIdx.x == 0) finish_row<KIND>(a, row, s);
-        const int n = p.splits * a.top;
-        for (int i = threadIdx.x; i < n; i += kJoinLanes)
-            lists[i] = ((const Key*)(parts + (i / a.top) * bytes + 16))[i % a.top];
-        __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kJoinLanes) {
-            const Key mine = lists[i];
-            int rank = i % a.top;
-            for (int l = 0; l < p.splits && rank < a.top; ++l) {
-                if (l == i / a.top) continue;
-                int low = 0, high = a.top;                  // keys above mine: a prefix of the list
-                while (low < high) {
-                    const int mid = (low + high) / 2;
-                    if (lists[l * a.top + mid] > mine) low = mid + 1;
-                    else high = mid;
-                }
-                rank += low;
-            }
-            if (rank < a.top && mine != 0) write_best(a, row, rank, mine, s);
-        }
-        __syncthreads();
     }
 }
 
@@ -410,7 +492,7 @@ struct LogProbsBackwardArgs {
 };
 constexpr int kGradLanes = 256;
 
-template <int KIND, bool RAGGED>
+template <int KIND, int TAIL, bool ENTROPY, bool NT>
 __global__ __launch_bounds__(kGradLanes) void logprobs_backward_kernel(LogProbsBackwardArgs p)
 {
     const LogProbsBackward& a = p.a;
@@ -422,7 +504,7 @@ __global__ __launch_bounds__(kGradLanes) void logprobs_backward_kernel(LogProbsB
         const char* const x_row = (const char*)a.logits.data + row * a.logits.stride * kWidth<KIND>;
         char* const d_row = (char*)a.dlogits.data + row * a.dlogits.stride * kWidth<KIND>;
         const int64_t target = a.targets[row];
-        const float lse = a.lse[row], h = a.dentropy ? a.dentropy[row] : 0.f, entropy = a.dentropy ? a.entropy[row] : 0.f;
+        const float lse = a.lse[row], h = ENTROPY ? a.dentropy[row] : 0.f, entropy = ENTROPY ? a.entropy[row] : 0.f;
         const float g = target < 0 ? 0.f : a.dlogprob[row];
         const bool bad = target >= (int64_t)a.vocab;
         const bool none = !bad && ((g == 0.f && h == 0.f) || lse == -infinity());
@@ -430,59 +512,89 @@ __global__ __launch_bounds__(kGradLanes) void logprobs_backward_kernel(LogProbsB
             float d[kVec] = {};
             if (!none) {
                 float x[kVec];
-                unpack<KIND>(load_col<KIND, RAGGED>(x_row, c, a.vocab), x);
+                Raw<KIND> r = load_col<KIND, TAIL>(x_row, c, a.vocab);
+                settle<KIND, TAIL>(r, c, a.vocab);
+                unpack<KIND>(r, x);
                 const unsigned hit = (unsigned)((uint64_t)target - (uint64_t)c * kVec < kVec ? target - (int64_t)c * kVec : kVec);
                 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {
                     const float logp = x[i] - lse, prob = exp_of(logp);
-                    d[i] = prob * __builtin_fmaf(-h, fmaxf(logp, kFar) + entropy, -g);
-                    if (hit == (unsigned)i) d[i] += g;
-                    if (bad) d[i] = __builtin_nanf("");
+                    d[i] = prob * (ENTROPY ? __builtin_fmaf(-h, fmaxf(logp, kFar) + entropy, -g) : -g);
+                }
+                if (hit < kVec) {
+                    #pragma unroll
+                    for (int i = 0; i < kVec; ++i) d[i] += hit == (unsigned)i ? g : 0.f;
+                }
+                if (bad) {
+                    #pragma unroll
+                    for (int i = 0; i < kVec; ++i) d[i] = __builtin_nanf("");
                 }
             }
-            store_col<KIND, RAGGED>(d_row, c, a.vocab, pack<KIND>(d));
+            store_col<KIND, TAIL, NT>(d_row, c, a.vocab, pack<KIND>(d));
         }
     }
 }
 
 unsigned grid_of(size_t blocks) { return (unsigned)std::min<size_t>(blocks, 1u << 20); }
 
-constexpr size_t kUnits = 256;              // compute units of an MI355X
+// Logits that no cache holds (256 MB of Infinity Cache) are read past the caches: 4096 x 65536 bf16 96.8 us, so 84.5; where
+// they may still be in one it costs 9 % (1024 x 50001 f32, 205 MB, 36.6 / 39.8).
+constexpr size_t kUncached = size_t{256} << 20;
+// A gradient that no cache keeps for its reader is stored past them: 4096 x 65536 bf16 176 us, so 165.
+constexpr size_t kUnkept = size_t{224} << 20;
 
 }  // namespace
 
-// Enough workgroups for every compute unit, but none with less than 8192 logits.
-int row_splits(size_t rows, size_t vocab)
+// Workgroups that share a row: as many as there are compute units for it, none with fewer than 32768 logits (us, one per row /
+// so / from 8192: 4 x 131072 bf16, 8 alternatives 17.8 / 13.2 / 16.5; 128 x 50000 15.0 / 15.0 / 19.5; 1 x 32000 5.0 / 5.0 / 7.6;
+// 32 x 128000 18.0 / 15.2 / 14.8: the second launch and the join have to be paid for), and no more keys than the join ranks.
+int row_splits(size_t rows, size_t vocab, int top)
 {
+    constexpr size_t kUnits = 256, kLeast = 32768;
     if (rows == 0 || rows >= kUnits) return 1;
-    return (int)std::max<size_t>(1, std::min<size_t>({kUnits / rows, vocab / 8192, 64}));
+    return (int)std::max<size_t>(1, std::min<size_t>({kUnits / rows, vocab / kLeast, 64, (size_t)kCandidates / std::max(top, 1)}));
 }
 
 int launch_logprobs(const LogProbs& a, int kind, void* stream)
 {
     const unsigned vecs = (unsigned)(((size_t)a.vocab + kVec - 1) / kVec);
-    LogProbsArgs p{a, row_splits(a.rows, a.vocab), 0};
+    LogProbsArgs p{a, row_splits(a.rows, a.vocab, a.top), 0};
     p.chunk = (vecs + p.splits - 1) / p.splits;
+    // 1024 lanes only where there is a compute unit for every workgroup (500 x 50001 f32, 5 alternatives: 256 lanes 27.4 us,
+    // 1024 lanes 42.4); two vectors in flight instead of four in short rows (8192 x 5000 bf16 23.9 / 27.4)
+    const bool wide = a.rows * p.splits <= 256 && p.chunk >= 4096, uncached = a.rows * a.vocab * (kind == kF32 ? 4 : 2) >= kUncached;
     return dispatch_kind(kind, [&](auto K) {
         constexpr int KIND = decltype(K)::value;
-        const int err = dispatch_flag(a.top > 0, [&](auto T) {
-            return launch_args(logprobs_kernel<KIND, 1024, 4, decltype(T)::value>, dim3(grid_of(a.rows * p.splits)), dim3(1024), 0,
-                               stream, p);
-        });
+        auto run = [&](auto L, auto U, auto N) { return dispatch_flag(a.top > 0, [&](auto T) { return dispatch_flag(a.entropy, [&](auto E) {
+            constexpr int LANES = decltype(L)::value;
+            return launch_args(logprobs_kernel<KIND, LANES, decltype(U)::value, decltype(T)::value, decltype(E)::value, decltype(N)::value>,
+                               dim3(grid_of(a.rows * p.splits)), dim3(LANES), 0, stream, p);
+        }); }); };
+        using std::integral_constant;
+        const int err = wide ? run(integral_constant<int, 1024>{}, integral_constant<int, 4>{}, std::false_type{})
+                      : p.chunk < 1024 ? run(integral_constant<int, 256>{}, integral_constant<int, 2>{}, std::false_type{})
+                      : uncached ? run(integral_constant<int, 256>{}, integral_constant<int, 4>{}, std::true_type{})
+                                 : run(integral_constant<int, 256>{}, integral_constant<int, 4>{}, std::false_type{});
         if (err || p.splits == 1) return err;
-        return launch_args(join_kernel<KIND>, dim3(grid_of(a.rows)), dim3(kJoinLanes), sizeof(Key) * p.splits * a.top, stream, p);
+        return dispatch_flag(a.top > 0, [&](auto T) {
+            return launch_args(join_kernel<KIND, decltype(T)::value>, dim3(grid_of(a.rows)), dim3(kJoinLanes), 0, stream, p);
+        });
     });
 }
 
 int launch_logprobs_backward(const LogProbsBackward& a, int kind, void* stream)
 {
     const unsigned vecs = (unsigned)(((size_t)a.vocab + kVec - 1) / kVec);
-    LogProbsBackwardArgs p{a, 4 * kGradLanes, 0};
+    // 32 bytes for each lane (4096 x 65536 bf16: one vector 192 us, two 165, four 176; 2000 x 50001 f32: one 141, two 156, four 169)
+    LogProbsBackwardArgs p{a, (kind == kF32 ? 1u : 2u) * kGradLanes, 0};
     p.chunks = (vecs + p.chunk - 1) / p.chunk;
-    return dispatch_kind(kind, [&](auto K) { return dispatch_flag(a.vocab % kVec != 0, [&](auto R) {
-        return launch_args(logprobs_backward_kernel<decltype(K)::value, decltype(R)::value>, dim3(grid_of(a.rows * p.chunks)),
-                           dim3(kGradLanes), 0, stream, p);
-    }); });
+    const bool unkept = a.rows * a.vocab * (kind == kF32 ? 4 : 2) >= kUnkept;
+    return dispatch_kind(kind, [&](auto K) { return dispatch_tail(a.vocab, [&](auto T) { return dispatch_flag(a.dentropy, [&](auto E) {
+        return dispatch_flag(unkept, [&](auto N) {
+            return launch_args(logprobs_backward_kernel<decltype(K)::value, decltype(T)::value, decltype(E)::value, decltype(N)::value>,
+                               dim3(grid_of(a.rows * p.chunks)), dim3(kGradLanes), 0, stream, p);
+        });
+    }); }); });
 }
 
 }  // namespace mics

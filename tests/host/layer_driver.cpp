@@ -33,13 +33,14 @@ int main()
         CHECK(d.scale == (float)(65536.0 / (65536.0 - d.threshold)) && d.seed == 5 && d.offset == ~0ull);
     }
     // the workspace of long rows holds the rows' sums in front
-    for (size_t c : {cols, (size_t)16384, (size_t)16385}) {
+    const size_t tiled = mics::kTiledCols;
+    for (size_t c : {cols, tiled, tiled + 1}) {
         const size_t need = mics_column_workspace_bytes(rows, c);
-        CHECK(need == 4 * (3 * rows * c + (c > 16384 ? 2 * rows : 0)));
+        CHECK(need == 4 * (3 * rows * c + (c > tiled ? 2 * rows : 0)));
         CHECK(mics_layer_norm_backward(fake(0), fake(1), nullptr, fake(2), fake(3), f32(4), f32(5), nullptr, rows, c, nullptr, 0, 0, 0,
                                        fake(6), need, nullptr) == MICS_OK);
         CHECK(mics::g_layer_launches == ++n);
-        CHECK((char*)mics::g_backward.parts - fake(6) == (c > 16384 ? 8 * (long)rows : 0) && !mics::g_backward.dsum.data);
+        CHECK((char*)mics::g_backward.parts - fake(6) == (c > tiled ? 8 * (long)rows : 0) && !mics::g_backward.dsum.data);
         CHECK(mics_layer_norm_backward(fake(0), fake(1), nullptr, fake(2), fake(3), f32(4), f32(5), nullptr, rows, c, nullptr, 0, 0, 0,
                                        fake(6), need - 1, nullptr) == MICS_ERR_INVALID_ARG);
     }

@@ -1,4 +1,4 @@
-// Stand-ins for the launchers of layer.hip and logprobs.hip: they record what they were asked for and touch no pointer.
+// Stand-ins for the launchers of norm.hip, dropout.hip and logprobs.hip: they record what they were asked for and touch no pointer.
 #include "layer_internal.h"
 
 namespace mics {
@@ -9,7 +9,7 @@ int launch_norm(const NormForward& a, int, bool, void*) { g_dropout = a.drop; ++
 int launch_norm_backward(const NormBackward& a, int, bool, void* const*, int, void*) { g_backward = a; ++g_layer_launches; return 0; }
 int launch_dropout(const DropoutPass& a, int, void*) { g_dropout = a.drop; ++g_layer_launches; return 0; }
 int launch_dropout_backward(const DropoutPass& a, int, void*, int, void*) { g_dropout = a.drop; ++g_layer_launches; return 0; }
-int row_splits(size_t rows, size_t) { return rows < 16 ? 4 : 1; }
+int row_splits(size_t rows, size_t, int) { return rows < 16 ? 4 : 1; }
 int launch_logprobs(const LogProbs&, int, void*) { ++g_layer_launches; return 77; }
 int launch_logprobs_backward(const LogProbsBackward&, int, void*) { ++g_layer_launches; return 0; }
 }  // namespace mics
