@@ -62,6 +62,8 @@ __global__ __launch_bounds__(kSumLanes) void column_sums_kernel(ColumnSumsArgs p
 struct DropoutArgs {
     DropoutPass a;
     size_t groups;        // vectors, and generator blocks, of a row
+    void* dbias;          // where a stripe has one workgroup, it stores the sums themselves
+    int grad;
 };
 // Single wavefronts (us, 64 / 256 / 512 lanes: 4096 x 8192 bf16 42.1 / 42.9 / 43.2, 4096 x 2560 13.1 / 13.6 / 14.1).
 constexpr int kDropLanes = 64;
@@ -140,7 +142,10 @@ __global__ __launch_bounds__(64 * kStripeWaves) void dropout_backward_kernel(Dro
             #pragma unroll
             for (int i = 0; i < kVec; ++i) acc[i] += lds[w][i][lane];
         }
-        store_col<kF32, TAIL>((char*)(a.parts + (size_t)blockIdx.x * a.cols), c, a.cols, pack<kF32>(acc));
+        if (gridDim.x > 1) store_col<kF32, TAIL>((char*)(a.parts + (size_t)blockIdx.x * a.cols), c, a.cols, pack<kF32>(acc));
+        else if (p.grad == kBf16) store_col<kBf16, TAIL>((char*)p.dbias, c, a.cols, pack<kBf16>(acc));
+        else if (p.grad == kF16) store_col<kF16, TAIL>((char*)p.dbias, c, a.cols, pack<kF16>(acc));
+        else store_col<kF32, TAIL>((char*)p.dbias, c, a.cols, pack<kF32>(acc));
     }
 }
 
@@ -155,7 +160,7 @@ int launch_column_sums(const float* parts, int sums, int groups, size_t cols, vo
 
 int launch_dropout(const DropoutPass& a, int kind, void* stream)
 {
-    const DropoutArgs p{a, vectors(a.cols)};
+    const DropoutArgs p{a, vectors(a.cols), nullptr, 0};
     return dispatch_kind(kind, [&](auto K) { return dispatch_tail(a.cols, [&](auto T) {
         return launch_args(dropout_kernel<decltype(K)::value, decltype(T)::value>,
                            dim3(grid_of((a.rows * p.groups + kDropLanes - 1) / kDropLanes)), dim3(kDropLanes), 0, stream, p);
@@ -164,15 +169,18 @@ int launch_dropout(const DropoutPass& a, int kind, void* stream)
 
 int launch_dropout_backward(const DropoutPass& a, int kind, void* dbias, int grad, void* stream)
 {
-    const DropoutArgs p{a, vectors(a.cols)};
+    const DropoutArgs p{a, vectors(a.cols), dbias, grad};
     const size_t stripes = (p.groups + 63) / 64;
     const size_t want = std::max<size_t>(1, kStripeBlocks * kUnits / stripes);
-    const int groups = (int)std::min({want, 2 * kMostParts, (a.rows + kStripeWaves - 1) / kStripeWaves});
+    // few rows: one workgroup for each stripe, and no second launch (us, two / one: 4 x 4096 7.5 / 4.7, 32 x 4096 7.4 / 5.0,
+    // 64 x 4096 7.3 / 7.9)
+    const bool one = a.rows > 0 && (a.rows <= 4 * kStripeWaves * kStripeRows || want == 1);
+    const int groups = one ? 1 : (int)std::min({want, 2 * kMostParts, (a.rows + kStripeWaves - 1) / kStripeWaves});
     const int err = a.rows == 0 ? 0 : dispatch_kind(kind, [&](auto K) { return dispatch_tail(a.cols, [&](auto T) {
         return launch_args(dropout_backward_kernel<decltype(K)::value, decltype(T)::value>,
                            dim3((unsigned)groups, (unsigned)stripes), dim3(64 * kStripeWaves), 0, stream, p);
     }); });
-    return err ? err : launch_column_sums(a.parts, 1, groups, a.cols, &dbias, grad, stream);
+    return err || one ? err : launch_column_sums(a.parts, 1, groups, a.cols, &dbias, grad, stream);
 }
 
 }  // namespace mics

@@ -89,7 +89,7 @@ template <int LANES> struct LogProbsLds<LANES, true> {
     int count;
     Key best[kMostTop];
     Key wave_best[LANES / 64];
-    Key candidate[kCandidates];
+    Key candidate[kCandidates + 4];
 };
 
 struct LogProbsArgs {
@@ -215,10 +215,16 @@ template <int LANES> __device__ __forceinline__ void rank_candidates(LogProbsLds
         barrier_lds();
         n = lds.count;
     }
+    // behind the n: no key, so that four can be compared at a time
+    if (threadIdx.x < 4) lds.candidate[n + threadIdx.x] = 0;
+    barrier_lds();
     for (int i = threadIdx.x; i < n; i += LANES) {
         const Key mine = lds.candidate[i];
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += lds.candidate[j] > mine;
+        for (int j = 0; j < n; j += 4) {
+            #pragma unroll
+            for (int u = 0; u < 4; ++u) rank += lds.candidate[j + u] > mine;
+        }
         if (rank < top) lds.best[rank] = mine;
     }
 }
@@ -364,11 +370,21 @@ __global__ __launch_bounds__(LANES) void logprobs_kernel(LogProbsArgs p)
             for (int u = 0; u < U; ++u)
                 r[u] = load_vec<KIND, NT>(span.row + (size_t)min(from + u * LANES, whole - 1) * (kVec * kWidth<KIND>), kVec);
         };
-        auto keep = [&](const float* x, unsigned c) {
+        // a lane's logits that reach the threshold: one place in the list for each, all of them at once
+        auto keep = [&](auto N, const float* x, unsigned c) {
             if constexpr (TOP) {
+                constexpr int VECS = decltype(N)::value;
+                int count = 0;
                 #pragma unroll
-                for (int i = 0; i < kVec; ++i)
-                    if (!(x[i] < threshold)) keep_candidate(lds, x[i], c * kVec + i);
+                for (int i = 0; i < VECS * kVec; ++i) count += !(x[i] < threshold);
+                if (count == 0) return;
+                int to = atomicAdd(&lds.count, count);
+                #pragma unroll
+                for (int i = 0; i < VECS * kVec; ++i)
+                    if (!(x[i] < threshold)) {
+                        if (to < kCandidates) lds.candidate[to] = key_of(x[i], (c + i / kVec * LANES) * kVec + i % kVec);
+                        ++to;
+                    }
             }
         };
         auto read = [&](auto PART, const Raw<KIND> (&r)[U], unsigned c, float (&x)[U * kVec]) {
@@ -382,10 +398,7 @@ __global__ __launch_bounds__(LANES) void logprobs_kernel(LogProbsArgs p)
             }
         };
         auto add = [&](const float (&x)[U * kVec], float most, unsigned c) {
-            if (TOP && !(most < threshold)) {
-                #pragma unroll
-                for (int u = 0; u < U; ++u) keep(x + u * kVec, c + u * LANES);
-            }
+            if (TOP && !(most < threshold)) keep(std::integral_constant<int, U>{}, x, c);
             add_logits<ENTROPY>(s, x, most);
         };
         if constexpr (TOP)
@@ -427,7 +440,7 @@ __global__ __launch_bounds__(LANES) void logprobs_kernel(LogProbsArgs p)
             float x[kVec];
             span.vec(whole, x);
             add_logits<ENTROPY>(s, x, largest(x));
-            keep(x, whole);
+            keep(std::integral_constant<int, 1>{}, x, whole);
         }
         s = block_stat<LANES>(lds.stat, s);
         if constexpr (TOP) {

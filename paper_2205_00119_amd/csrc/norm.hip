@@ -121,9 +121,9 @@ __global__ __launch_bounds__(LANES) void norm_kernel(NormForwardArgs p)
                 if (l == 0) parts[turn][wave] = {mean, square};
                 barrier_lds();
                 const float2 part = l < p.waves ? parts[turn][l] : float2{0.f, 0.f};
-                mean = wave_sum(others * part.x) / n;
+                mean = sum_of_16(others * part.x) / n;
                 const float d = part.x - mean;
-                square = wave_sum(__builtin_fmaf(others * d, d, part.y));
+                square = sum_of_16(__builtin_fmaf(others * d, d, part.y));
                 turn ^= 1;
             }
             const float rstd = 1.f / __builtin_sqrtf(square / n + a.eps);
@@ -163,7 +163,7 @@ __device__ __forceinline__ float2 row_sum(RowSums& lds, int turn, int wave, int 
     if (lane == 0) slot[wave] = s;
     barrier_lds();
     s = lane < waves ? slot[first + lane] : float2{0.f, 0.f};
-    return {wave_sum(s.x), wave_sum(s.y)};
+    return {sum_of_16(s.x), sum_of_16(s.y)};
 }
 
 // Rows that no workgroup's registers hold: three passes over them, the second and third from the caches.
@@ -231,6 +231,8 @@ struct NormBackwardArgs {
     NormBackward a;
     size_t groups;
     int waves, batch;
+    void* grads[3];       // where one workgroup has all rows, it stores the sums themselves
+    int grad;
 };
 
 // What the loop must not skip is as in the forward pass (dresidual: dx, stored over).  TILED: s1 and s2 come from
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(LANES) void norm_backward_kernel(NormBackwardArgs p
     // PART: `mine` is false in wavefronts past the last row, which pass the barrier only
     auto work = [&](auto PART, Row& now, size_t row, bool mine) {
         constexpr bool ALL = !decltype(PART)::value;
-        float s1 = 0.f, s2 = 0.f;
+        float s1 = 0.f, s2 = 0.f, hat[V][kVec], d[V][kVec];
         if (ALL || mine) {
             #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -306,13 +308,14 @@ __global__ __launch_bounds__(LANES) void norm_backward_kernel(NormBackwardArgs p
                 unpack<KIND>(now.x[v], x);
                 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {
-                    const float hat = (x[i] - now.mean) * now.rstd;
-                    acc[0][v][i] = __builtin_fmaf(dy[i], hat, acc[0][v][i]);
+                    hat[v][i] = (x[i] - now.mean) * now.rstd;
+                    d[v][i] = dy[i] * w[v][i];
+                    acc[0][v][i] = __builtin_fmaf(dy[i], hat[v][i], acc[0][v][i]);
                     acc[1][v][i] += dy[i];
                     if constexpr (!TILED) {
-                        const float d = at.element(dy[i] * w[v][i], i);
-                        p1 += d;
-                        p2 = __builtin_fmaf(d, hat, p2);
+                        const float own = at.element(d[v][i], i);
+                        p1 += own;
+                        p2 = __builtin_fmaf(own, hat[v][i], p2);
                     }
                 }
                 s1 += at.vector(p1);
@@ -330,17 +333,13 @@ __global__ __launch_bounds__(LANES) void norm_backward_kernel(NormBackwardArgs p
             turn ^= 1;
         }
         if (ALL || mine) {
-            const float c1 = s.x * over, c2 = s.y * over;
+            // rstd (d - c1 - hat c2)
+            const float c1 = -(now.rstd * over) * s.x, c2 = -(now.rstd * over) * s.y;
             #pragma unroll
             for (int v = 0; v < V; ++v) {
-                float dy[kVec], x[kVec], ds[kVec];
-                unpack<KIND>(now.dy[v], dy);
-                unpack<KIND>(now.x[v], x);
+                float ds[kVec];
                 #pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    const float hat = (x[i] - now.mean) * now.rstd;
-                    ds[i] = now.rstd * ((dy[i] * w[v][i] - c1) - hat * c2);
-                }
+                for (int i = 0; i < kVec; ++i) ds[i] = __builtin_fmaf(hat[v][i], c2, __builtin_fmaf(d[v][i], now.rstd, c1));
                 if constexpr (MODE == kBlockSum) {
                     float t[kVec];
                     unpack<KIND>(now.dsum[v], t);
@@ -393,7 +392,12 @@ __global__ __launch_bounds__(LANES) void norm_backward_kernel(NormBackwardArgs p
                     for (int j = 0; j < V * kVec; ++j) acc[k][j / kVec][j % kVec] += other[j * lanes + lane];
                 }
         }
-        if (group == 0) {
+        if (group == 0 && !TILED && gridDim.x == 1) {
+            if (p.grads[k]) {
+                #pragma unroll
+                for (int v = 0; v < V; ++v) place(v).round(p.grads[k], p.grad, acc[k][v]);
+            }
+        } else if (group == 0) {
             float* const part = a.parts + ((size_t)k * gridDim.x + blockIdx.x) * a.cols;
             #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -482,8 +486,9 @@ int launch_norm_backward(const NormBackward& given, int kind, bool fused, void* 
     NormBackward a = given;
     if (!a.dresidual.data) a.dresidual = a.dx;
     const size_t vecs = vectors(a.cols);
-    NormBackwardArgs p{a, vecs, 1, 1};
+    NormBackwardArgs p{a, vecs, 1, 1, {grads[0], grads[1], fused ? grads[2] : nullptr}, grad};
     int groups = 0;
+    bool sums = true;
     // no row: the gradients of the parameters are zero
     const int err = a.rows == 0 ? 0 : dispatch_kind(kind, [&](auto K) {
         constexpr int KIND = decltype(K)::value;
@@ -494,7 +499,11 @@ int launch_norm_backward(const NormBackward& given, int kind, bool fused, void* 
                 return dispatch_tail<!decltype(TT)::value>(a.cols, [&](auto T) {
                     p.waves = waves_of(std::min<size_t>(vecs, (size_t)LANES * V), V);
                     p.batch = LANES / 64 / p.waves;
-                    groups = (int)std::min<size_t>(kMostParts, (a.rows + p.batch - 1) / p.batch);
+                    // few rows: one workgroup, and no second launch (us, two / one: 1 x 2560 8.2 / 4.9, 8 x 2560 in three batches 7.8 / 7.1,
+                    // 4 x 8192 in four 7.7 / 7.7)
+                    const bool one = !decltype(TT)::value && a.rows <= 2 * (size_t)p.batch;
+                    sums = !one;
+                    groups = one ? 1 : (int)std::min<size_t>(kMostParts, (a.rows + p.batch - 1) / p.batch);
                     const size_t lds = (size_t)(p.batch - 1) * 64 * p.waves * V * kVec * 4;
                     const size_t tile = (size_t)64 * p.waves * V;
                     return launch_args(norm_backward_kernel<KIND, V, MODE, decltype(T)::value, BUFFERS, decltype(TT)::value, LANES>,
@@ -515,7 +524,7 @@ int launch_norm_backward(const NormBackward& given, int kind, bool fused, void* 
         if (!a.dsum.data) return mode(Int<kBlock>{});
         return mode(Int<kBlockSum>{});
     });
-    return err ? err : launch_column_sums(a.parts, fused ? 3 : 2, groups, a.cols, grads, grad, stream);
+    return err || !sums ? err : launch_column_sums(a.parts, fused ? 3 : 2, groups, a.cols, grads, grad, stream);
 }
 
 }  // namespace mics

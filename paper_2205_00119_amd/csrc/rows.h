@@ -260,11 +260,18 @@ template <int TAIL> struct Place {
     __device__ __forceinline__ float columns() const { return (float)max(kVec - out, 0); }
     template <int KIND> __device__ __forceinline__ Raw<KIND> load(const char* row) const
     {
-        return load_vec<KIND>(row + (size_t)e * kWidth<KIND>, TAIL == kTiny ? kVec - out : kVec);
+        return load_vec<KIND>(row + e * (unsigned)kWidth<KIND>, TAIL == kTiny ? kVec - out : kVec);
     }
     template <int KIND> __device__ __forceinline__ void store(char* row, const Raw<KIND>& r) const
     {
-        store_vec<KIND>(row + (size_t)e * kWidth<KIND>, r, TAIL == kTiny ? kVec - out : kVec);
+        store_vec<KIND>(row + e * (unsigned)kWidth<KIND>, r, TAIL == kTiny ? kVec - out : kVec);
+    }
+    // Stored in a kind known at run time (the same in all lanes).
+    __device__ __forceinline__ void round(void* p, int kind, const float (&v)[kVec]) const
+    {
+        if (kind == kBf16) store<kBf16>((char*)p, pack<kBf16>(v));
+        else if (kind == kF16) store<kF16>((char*)p, pack<kF16>(v));
+        else store<kF32>((char*)p, pack<kF32>(v));
     }
     // A parameter of a kind known at run time (the same in all lanes); NULL: `absent` everywhere.
     __device__ __forceinline__ void param(const void* p, int kind, float absent, float (&v)[kVec]) const
@@ -311,6 +318,16 @@ __device__ __forceinline__ float wave_sum(float v)
     v += dpp_zero<0x142, 0xA>(v);          // row_bcast:15 into rows 1 and 3
     v += dpp_zero<0x143, 0xC>(v);          // row_bcast:31 into rows 2 and 3
     return lane_value(v, 63);
+}
+
+// The sum of the first 16 lanes, in all lanes.
+__device__ __forceinline__ float sum_of_16(float v)
+{
+    v += dpp_zero<0x111, 0xF>(v);
+    v += dpp_zero<0x112, 0xF>(v);
+    v += dpp_zero<0x114, 0xF>(v);
+    v += dpp_zero<0x118, 0xF>(v);
+    return lane_value(v, 15);
 }
 
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3", 2011) of the counter
