@@ -370,21 +370,19 @@ __global__ __launch_bounds__(LANES) void logprobs_kernel(LogProbsArgs p)
             for (int u = 0; u < U; ++u)
                 r[u] = load_vec<KIND, NT>(span.row + (size_t)min(from + u * LANES, whole - 1) * (kVec * kWidth<KIND>), kVec);
         };
-        // a lane's logits that reach the threshold: one place in the list for each, all of them at once
+        // a lane's logits that reach the threshold, by index: one place in the list for each, all of them at once
         auto keep = [&](auto N, const float* x, unsigned c) {
             if constexpr (TOP) {
-                constexpr int VECS = decltype(N)::value;
-                int count = 0;
+                constexpr int COUNT = decltype(N)::value * kVec;
+                uint32_t reached = 0;
                 #pragma unroll
-                for (int i = 0; i < VECS * kVec; ++i) count += !(x[i] < threshold);
-                if (count == 0) return;
-                int to = atomicAdd(&lds.count, count);
-                #pragma unroll
-                for (int i = 0; i < VECS * kVec; ++i)
-                    if (!(x[i] < threshold)) {
-                        if (to < kCandidates) lds.candidate[to] = key_of(x[i], (c + i / kVec * LANES) * kVec + i % kVec);
-                        ++to;
-                    }
+                for (int i = 0; i < COUNT; ++i) reached |= x[i] < threshold ? 0u : 1u << i;
+                if (!reached) return;
+                int to = atomicAdd(&lds.count, __popc(reached));
+                for (; reached; reached &= reached - 1, ++to) {
+                    const unsigned i = __builtin_ctz(reached);
+                    if (to < kCandidates) lds.candidate[to] = (c + i / kVec * LANES) * kVec + i % kVec;
+                }
             }
         };
         auto read = [&](auto PART, const Raw<KIND> (&r)[U], unsigned c, float (&x)[U * kVec]) {
@@ -447,6 +445,13 @@ __global__ __launch_bounds__(LANES) void logprobs_kernel(LogProbsArgs p)
             const int n = lds.count;      // behind block_stat's barrier
             barrier_lds();              // and before it is set back
             if (s.z == s.z && n <= kCandidates) {
+                // a register cannot be chosen by a number, so their logits are read again
+                for (int i = threadIdx.x; i < n; i += LANES) {
+                    const unsigned index = (unsigned)lds.candidate[i];
+                    const char* const from = span.row + (size_t)index * kWidth<KIND>;
+                    lds.candidate[i] = key_of(KIND == kF32 ? *(const float*)from : widen<KIND>(*(const uint16_t*)from), index);
+                }
+                barrier_lds();
                 rank_candidates<LANES>(lds, n, a.top);
                 if (masked && n < a.top && threadIdx.x < 64) fill_equal<KIND, LANES>(lds, span, n, a.top, -infinity());
             } else {
