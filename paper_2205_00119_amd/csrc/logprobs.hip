@@ -348,8 +348,10 @@ __device__ __forceinline__ void write_best(const LogProbs& a, size_t row, int k,
 
 // One pass: U vectors of every lane are worked on while the next U are loaded.  TOP: the first U tell a threshold, and what
 // reaches it is kept as a candidate on the way.
+// Four wavefronts for each unit of a compute unit where that spills nothing (2048 x 32768 bf16, 5 alternatives: three 41.9 us, four
+// 38.8; of 32-bit logits, which spill, 500 x 50001 22.1 / 25.7).
 template <int KIND, int LANES, int U, bool TOP, bool ENTROPY, bool NT>
-__global__ __launch_bounds__(LANES) void logprobs_kernel(LogProbsArgs p)
+__global__ __launch_bounds__(LANES, LANES == 256 && U == 4 && TOP && KIND != kF32 ? 4 : 1) void logprobs_kernel(LogProbsArgs p)
 {
     const LogProbs& a = p.a;
     __shared__ LogProbsLds<LANES, TOP> lds;
@@ -579,7 +581,8 @@ int launch_logprobs(const LogProbs& a, int kind, void* stream)
     LogProbsArgs p{a, row_splits(a.rows, a.vocab, a.top), 0};
     p.chunk = (vecs + p.splits - 1) / p.splits;
     // 1024 lanes only where there is a compute unit for every workgroup (500 x 50001 f32, 5 alternatives: 256 lanes 27.4 us,
-    // 1024 lanes 42.4); two vectors in flight instead of four in short rows (8192 x 5000 bf16 23.9 / 27.4)
+    // 1024 lanes 42.4); two vectors in flight instead of four in short rows (8192 x 5000 bf16 23.9 / 27.4; 3475 x 9296 binary16,
+    // 20 alternatives, 38.0 / 44.0)
     const bool wide = a.rows * p.splits <= 256 && p.chunk >= 4096, uncached = a.rows * a.vocab * (kind == kF32 ? 4 : 2) >= kUncached;
     return dispatch_kind(kind, [&](auto K) {
         constexpr int KIND = decltype(K)::value;
@@ -590,7 +593,7 @@ int launch_logprobs(const LogProbs& a, int kind, void* stream)
         }); }); };
         using std::integral_constant;
         const int err = wide ? run(integral_constant<int, 1024>{}, integral_constant<int, 4>{}, std::false_type{})
-                      : p.chunk < 1024 ? run(integral_constant<int, 256>{}, integral_constant<int, 2>{}, std::false_type{})
+                      : p.chunk < (a.top ? 2048 : 1024) ? run(integral_constant<int, 256>{}, integral_constant<int, 2>{}, std::false_type{})
                       : uncached ? run(integral_constant<int, 256>{}, integral_constant<int, 4>{}, std::true_type{})
                                  : run(integral_constant<int, 256>{}, integral_constant<int, 4>{}, std::false_type{});
         if (err || p.splits == 1) return err;
