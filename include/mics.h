@@ -17,6 +17,11 @@
  *   mics_adam_shard            mixed-precision Adam on the rank's shard of the
  *                              model states (Sections 2.1 and 3.2)
  *
+ * and, in the last part of this header, operators that the rank runs on the
+ * gathered parameters before there is a gradient to reduce: layer norm,
+ * dropout with bias and residual, both in one pass, and token log
+ * probabilities, each forward and backward.
+ *
  * Notation (paper Section 3.1): k = devices per node, p = devices holding one
  * model replica (partition group size), s = micro-steps.  r = size of a
  * replication group (Section 3.2).  Group rank g sits on node j = g div k with

@@ -3,6 +3,12 @@
 // Every byte is read once and written once: a row stays in the registers of the lanes that read it, from the load to the
 // last store.  Bound by HBM bandwidth at large sizes, by launches and reductions at small ones.  Workgroups stay on their
 // compute unit and go from row to row; the loads of the next row are in flight while one is worked on.
+//
+// Measured on one MI355X, bf16, three sets of buffers in turn: forward 8192 x 8192 49.2 us = 5.46 TB/s (HBM traffic equal to the
+// algorithmic bytes), with bias, dropout and residual 4096 x 5120 36.1 us = 4.65 TB/s; backward 4096 x 4096 25.4 us, 20 of them in
+// the first kernel (5.0 TB/s), with all there is 4096 x 8192 74.0 us = 4.5 TB/s, 67 in the first.  Results are left to the caches
+// for whoever reads them next: stored past them the forward pass is up to 20 % shorter by itself (4096 x 5120 28.5 us), but
+// with the kernels that read y and sum behind it 4 % longer (69.2 / 71.9; 4096 x 4096 55.7 / 59.9).
 #include "rows.h"
 
 #include <algorithm>
