@@ -567,12 +567,13 @@ constexpr size_t kUnkept = size_t{224} << 20;
 
 }  // namespace
 
-// Workgroups that share a row: as many as there are compute units for it, none with fewer than 32768 logits (us, one per row /
-// so / from 8192: 4 x 131072 bf16, 8 alternatives 17.8 / 13.2 / 16.5; 128 x 50000 15.0 / 15.0 / 19.5; 1 x 32000 5.0 / 5.0 / 7.6;
-// 32 x 128000 18.0 / 15.2 / 14.8: the second launch and the join have to be paid for), and no more keys than the join ranks.
+// Workgroups that share a row: as many as there are compute units for it, none with fewer than 16384 logits (us, 8192 / so / 32768 /
+// 65536: 4 x 131072 bf16, 8 alternatives 12.9 / 12.5 / 12.6 / 14.8; 8 x 150000 6.3 / 6.8 / 9.0 / 10.9; 32 x 128000, 5 alternatives
+// 13.2 / 12.7 / 15.2 / 17.3; 1 x 32000 6.1 / 5.0 / 5.0 / 5.0: the second launch and the join have to be paid for), and no more
+// keys than the join ranks.
 int row_splits(size_t rows, size_t vocab, int top)
 {
-    constexpr size_t kUnits = 256, kLeast = 32768;
+    constexpr size_t kUnits = 256, kLeast = 16384;
     if (rows == 0 || rows >= kUnits) return 1;
     return (int)std::max<size_t>(1, std::min<size_t>({kUnits / rows, vocab / kLeast, 64, (size_t)kCandidates / std::max(top, 1)}));
 }
@@ -583,9 +584,10 @@ int launch_logprobs(const LogProbs& a, int kind, void* stream)
     LogProbsArgs p{a, row_splits(a.rows, a.vocab, a.top), 0};
     p.chunk = (vecs + p.splits - 1) / p.splits;
     // 1024 lanes only where there is a compute unit for every workgroup (500 x 50001 f32, 5 alternatives: 256 lanes 27.4 us,
-    // 1024 lanes 42.4); two vectors in flight instead of four in short rows (8192 x 5000 bf16 23.9 / 27.4; 3475 x 9296 binary16,
+    // 1024 lanes 42.4) and enough for each lane, less where it saves the join (1 x 32000 bf16 256 lanes 5.0, 1024 lanes 4.4;
+    // 4 x 131072 in eight parts 12.5 / 13.1); two vectors in flight instead of four in short rows (8192 x 5000 bf16 23.9 / 27.4; 3475 x 9296 binary16,
     // 20 alternatives, 38.0 / 44.0)
-    const bool wide = a.rows * p.splits <= 256 && p.chunk >= 4096, uncached = a.rows * a.vocab * (kind == kF32 ? 4 : 2) >= kUncached;
+    const bool wide = a.rows * p.splits <= 256 && p.chunk >= (p.splits == 1 ? 2048 : 4096), uncached = a.rows * a.vocab * (kind == kF32 ? 4 : 2) >= kUncached;
     return dispatch_kind(kind, [&](auto K) {
         constexpr int KIND = decltype(K)::value;
         auto run = [&](auto L, auto U, auto N) { return dispatch_flag(a.top > 0, [&](auto T) { return dispatch_flag(a.entropy, [&](auto E) {
