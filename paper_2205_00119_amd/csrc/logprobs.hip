@@ -5,7 +5,7 @@
 // so one pass that keeps (m, Z, T) and rescales them when m grows reads every logit once.  Z and T of two parts join as
 //     Z = Z1 e^(m1-m) + Z2 e^(m2-m),    T = sum of e^(mi-m) (Ti + (mi-m) Zi).
 // Bound by HBM bandwidth with many rows, by latency with few.  Measured on one MI355X: 4096 x 65536 bf16 with entropy 82.0 us =
-// 6.5 TB/s; 500 x 50001 f32 with 5 alternatives 22.3 us = 4.5 TB/s; 4 x 131072 bf16 with 8 12.5 us, two launches; the gradient of
+// 6.5 TB/s; 500 x 50001 f32 with 5 alternatives 22.4 us = 4.5 TB/s; 4 x 131072 bf16 with 8 12.5 us, two launches; the gradient of
 // 4096 x 65536 165.7 us, 6.2 TB/s of what it reads and writes.
 #include "rows.h"
 
