@@ -290,6 +290,7 @@ template <int KIND, int LANES> __device__ __forceinline__ void best_of_any(LogPr
         fill = true;
     }
     const int n = lds.count;
+    barrier_lds();       // and before it is set back
     if (n <= kCandidates) {
         rank_candidates<LANES>(lds, n, top);
         if (fill && wave == 0) fill_equal<KIND, LANES>(lds, span, n, top, threshold);

@@ -371,6 +371,15 @@ def test_logits_that_are_not_numbers(rows, cols):
     check_logprobs(all_nan, np.array([0, -1]), 4)
 
 
+@pytest.mark.parametrize("rows,cols,fmt", [(3, 1000, "f32"), (300, 3001, "bf16"), (2, 70001, "f16")])
+@pytest.mark.parametrize("share", [0.3, 0.6])
+def test_alternatives_among_many_that_are_not_numbers(rows, cols, fmt, share):
+    r = np.random.default_rng(11)
+    data = r.normal(size=(rows, cols))
+    data[r.random((rows, cols)) < share] = np.nan
+    check_logprobs(Matrix(rows, cols, fmt, data=data), targets_of(r, rows, cols), 20)
+
+
 def test_targets_outside_the_vocabulary():
     x = Matrix(3, 100, "f32", data=normal(1, 3, 100))
     t = np.array([100, 2 ** 40, -2 ** 40])
