@@ -6,7 +6,7 @@
 //     Z = Z1 e^(m1-m) + Z2 e^(m2-m),    T = sum of e^(mi-m) (Ti + (mi-m) Zi).
 // Bound by HBM bandwidth with many rows, by latency with few.  Measured on one MI355X: 4096 x 65536 bf16 with entropy 82.0 us =
 // 6.5 TB/s; 500 x 50001 f32 with 5 alternatives 22.4 us = 4.5 TB/s; 4 x 131072 bf16 with 8 12.5 us, two launches; the gradient of
-// 4096 x 65536 165.7 us, 6.2 TB/s of what it reads and writes.
+// 4096 x 65536 165.7 us = 6.5 TB/s read and written.
 #include "rows.h"
 
 #include <algorithm>
@@ -351,8 +351,8 @@ __device__ __forceinline__ void write_best(const LogProbs& a, size_t row, int k,
 
 // One pass: U vectors of every lane are worked on while the next U are loaded.  TOP: the first U tell a threshold, and what
 // reaches it is kept as a candidate on the way.
-// Four wavefronts for each unit of a compute unit where that spills nothing (2048 x 32768 bf16, 5 alternatives: three 41.9 us, four
-// 38.8; of 32-bit logits, which spill, 500 x 50001 22.1 / 25.7).
+// Four wavefronts for each unit of a compute unit where that spills nothing (2048 x 32768 bf16, 5 alternatives: three 42.0 us, four
+// 38.9; of 32-bit logits, which spill, 500 x 50001 22.2 / 25.8).
 template <int KIND, int LANES, int U, bool TOP, bool ENTROPY, bool NT>
 __global__ __launch_bounds__(LANES, LANES == 256 && U == 4 && TOP && KIND != kF32 ? 4 : 1) void logprobs_kernel(LogProbsArgs p)
 {
@@ -560,10 +560,10 @@ __global__ __launch_bounds__(kGradLanes) void logprobs_backward_kernel(LogProbsB
 
 unsigned grid_of(size_t blocks) { return (unsigned)std::min<size_t>(blocks, 1u << 20); }
 
-// Logits that no cache holds (256 MB of Infinity Cache) are read past the caches: 4096 x 65536 bf16 96.8 us, so 84.5; where
-// they may still be in one it costs 9 % (1024 x 50001 f32, 205 MB, 36.6 / 39.8).
+// Logits that no cache holds (256 MB of Infinity Cache) are read past the caches: 4096 x 65536 bf16 96.6 us, so 83.4; where
+// they may still be in one it costs 9 % (1024 x 50001 f32, 205 MB, 36.8 / 40.1).
 constexpr size_t kUncached = size_t{256} << 20;
-// A gradient that no cache keeps for its reader is stored past them: 4096 x 65536 bf16 176 us, so 165.
+// A gradient that no cache keeps for its reader is stored past them: 4096 x 65536 bf16 171.7 us, so 165.8.
 constexpr size_t kUnkept = size_t{224} << 20;
 
 }  // namespace
@@ -584,10 +584,10 @@ int launch_logprobs(const LogProbs& a, int kind, void* stream)
     const unsigned vecs = (unsigned)(((size_t)a.vocab + kVec - 1) / kVec);
     LogProbsArgs p{a, row_splits(a.rows, a.vocab, a.top), 0};
     p.chunk = (vecs + p.splits - 1) / p.splits;
-    // 1024 lanes only where there is a compute unit for every workgroup (500 x 50001 f32, 5 alternatives: 256 lanes 27.4 us,
-    // 1024 lanes 42.4) and enough for each lane, less where it saves the join (1 x 32000 bf16 256 lanes 5.0, 1024 lanes 4.4;
-    // 4 x 131072 in eight parts 12.5 / 13.1); two vectors in flight instead of four in short rows (8192 x 5000 bf16 23.9 / 27.4; 3475 x 9296 binary16,
-    // 20 alternatives, 38.0 / 44.0)
+    // 1024 lanes only where there is a compute unit for every workgroup (500 x 50001 f32, 5 alternatives: 256 lanes 22.2 us,
+    // 1024 lanes 43.7) and enough for each lane, less where it saves the join (1 x 32000 bf16 256 lanes 5.0, 1024 lanes 4.4;
+    // 4 x 131072 in eight parts 12.5 / 13.1); two vectors in flight instead of four in short rows (8192 x 5000 bf16 24.7 / 26.1;
+    // 3475 x 9296 binary16, 20 alternatives, 38.3 / 44.3)
     const bool wide = a.rows * p.splits <= 256 && p.chunk >= (p.splits == 1 ? 2048 : 4096), uncached = a.rows * a.vocab * (kind == kF32 ? 4 : 2) >= kUncached;
     return dispatch_kind(kind, [&](auto K) {
         constexpr int KIND = decltype(K)::value;
