@@ -116,9 +116,6 @@ template <int KIND> struct Span {
     }
 };
 
-// How far a logit may be above a lane's base before its sums are moved to a new one: e^8 costs no precision.
-constexpr float kSlack = 8.f;
-
 template <int N> __device__ __forceinline__ float largest(const float (&x)[N])
 {
     float most = -infinity();
@@ -126,9 +123,12 @@ template <int N> __device__ __forceinline__ float largest(const float (&x)[N])
     for (int i = 0; i < N; ++i) most = fmaxf(most, x[i]);
     return most;
 }
+// The base is the largest logit so far.  A lower one would do for Z, but log Z, T / Z and logits less the base would then be as large
+// as it is too low, and what they leave of each other -- the entropy, the log probability of what is almost certain -- would keep
+// their rounding alone.
 template <bool ENTROPY, int N> __device__ __forceinline__ void add_logits(Stat& s, const float (&x)[N], float most)
 {
-    if (__builtin_amdgcn_ballot_w64(most > s.base + kSlack)) s.move_to(fmaxf(most, s.base));
+    if (__builtin_amdgcn_ballot_w64(most > s.base)) s.move_to(fmaxf(most, s.base));
     #pragma unroll
     for (int i = 0; i < N; ++i) {
         const float d = x[i] - s.base, e = exp_of(d);
