@@ -1,4 +1,4 @@
-"""Digits of log probabilities that a bound on sums of order one cannot see: the small entropy of rows with little choice."""
+"""Digits of log probabilities that bounds on sums of order one cannot see: small entropies, gradients of far logits."""
 import numpy as np
 import pytest
 import torch
@@ -6,6 +6,8 @@ import torch
 from test_gpu_layer_ops import Matrix, run_logprobs
 
 pytestmark = pytest.mark.gpu
+
+mics = pytest.importorskip("paper_2205_00119_amd")
 
 U = 2.0 ** -24
 
@@ -45,3 +47,28 @@ def test_rows_with_two_outcomes(rows, cols, fmt, top, low, high):
         worst["second"] = np.abs(got["top"][:, 1] - of_low) / far
     worst = {k: float(v.max()) for k, v in worst.items()}
     assert max(worst.values()) <= 1, worst
+
+
+@pytest.mark.parametrize("rows,cols", [(5, 7), (300, 5003), (40, 20000)])
+@pytest.mark.parametrize("of_entropy", [False, True])
+@pytest.mark.parametrize("moved", [False, True])
+def test_gradient_of_far_logits_in_32_bits(rows, cols, of_entropy, moved):
+    """Probabilities down to e^-85.  x - lse is exact where lse is 0, else within U |x - lse|; the exponential is within 2 U and a
+    correction by U more, the factor (1, or x - lse with an entropy of 0) and the product are rounded once each."""
+    r = np.random.default_rng(rows + cols)
+    x = Matrix(rows, cols, "f32", data=-85.0 * r.random((rows, cols)))
+    shift = r.normal(size=rows).astype(np.float32) if moved else np.zeros(rows, np.float32)
+    up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to("cuda:0")              # noqa: E731
+    ones, none = np.ones(rows, np.float32), np.zeros(rows, np.float32)
+    # all targets in column 0, which is left out below
+    g, h = (none, ones) if of_entropy else (ones, none)
+    dx = Matrix(rows, cols, "f32")
+    mics.mics_token_logprobs_backward(dx.t, x.t, up(np.zeros(rows, np.int64)), up(shift), up(none) if of_entropy else None, up(g),
+                                      up(h) if of_entropy else None, rows, cols, dtype=mics.MICS_DTYPE_F32)
+    logp = x.f64() - shift.astype(np.float64)[:, None]
+    want = -np.exp(logp) * (logp if of_entropy else 1.0)
+    bound = U * (8 + (2 if of_entropy else 1) * moved * np.abs(logp)) * np.abs(want)
+    # a logarithm of a probability near 1 is itself the difference
+    bound += U * moved * np.abs(x.f64()) * np.exp(logp) * of_entropy
+    worst = float((np.abs(dx.f64() - want) / bound)[:, 1:].max())
+    assert worst <= 1, worst
