@@ -12,6 +12,7 @@
 #include <algorithm>
 
 #include "layer_internal.h"
+#include "logprobs_rules.h"
 
 namespace mics {
 namespace {
@@ -88,8 +89,6 @@ __device__ __forceinline__ float value_of(Key k)
     return __builtin_bit_cast(float, up & 0x80000000u ? up ^ 0x80000000u : ~up);
 }
 __device__ __forceinline__ unsigned index_of(Key k) { return 0xFFFFFFFFu - (uint32_t)k; }
-
-constexpr int kCandidates = 2048;
 
 template <int LANES, bool TOP> struct LogProbsLds {
     Stat stat[LANES / 64];
@@ -523,7 +522,6 @@ struct LogProbsBackwardArgs {
     LogProbsBackward a;
     unsigned chunk, chunks;      // vectors of a workgroup, workgroups of a row
 };
-constexpr int kGradLanes = 256;
 
 template <int KIND, int TAIL, bool ENTROPY, bool NT>
 __global__ __launch_bounds__(kGradLanes) void logprobs_backward_kernel(LogProbsBackwardArgs p)
@@ -570,35 +568,15 @@ __global__ __launch_bounds__(kGradLanes) void logprobs_backward_kernel(LogProbsB
 
 unsigned grid_of(size_t blocks) { return (unsigned)std::min<size_t>(blocks, 1u << 20); }
 
-// Logits that no cache holds (256 MB of Infinity Cache) are read past the caches: 4096 x 65536 bf16 96.6 us, so 83.4; where
-// they may still be in one it costs 9 % (1024 x 50001 f32, 205 MB, 36.8 / 40.1).
-constexpr size_t kUncached = size_t{256} << 20;
-// A gradient that no cache keeps for its reader is stored past them: 4096 x 65536 bf16 171.7 us, so 165.8.
-constexpr size_t kUnkept = size_t{224} << 20;
-
 }  // namespace
 
-// Workgroups that share a row: as many as there are compute units for it, none with fewer than 16384 logits (us, 8192 / so / 32768 /
-// 65536: 4 x 131072 bf16, 8 alternatives 12.9 / 12.5 / 12.6 / 14.8; 8 x 150000 6.3 / 6.8 / 9.0 / 10.9; 32 x 128000, 5 alternatives
-// 13.2 / 12.7 / 15.2 / 17.3; 1 x 32000 6.1 / 5.0 / 5.0 / 5.0: the second launch and the join have to be paid for), and no more
-// keys than the join ranks.
-int row_splits(size_t rows, size_t vocab, int top)
-{
-    constexpr size_t kUnits = 256, kLeast = 16384;
-    if (rows == 0 || rows >= kUnits) return 1;
-    return (int)std::max<size_t>(1, std::min<size_t>({kUnits / rows, vocab / kLeast, 64, (size_t)kCandidates / std::max(top, 1)}));
-}
+int row_splits(size_t rows, size_t vocab, int top) { return splits_of(rows, vocab, top); }
 
 int launch_logprobs(const LogProbs& a, int kind, void* stream)
 {
-    const unsigned vecs = (unsigned)(((size_t)a.vocab + kVec - 1) / kVec);
-    LogProbsArgs p{a, row_splits(a.rows, a.vocab, a.top), 0};
-    p.chunk = (vecs + p.splits - 1) / p.splits;
-    // 1024 lanes only where there is a compute unit for every workgroup (500 x 50001 f32, 5 alternatives: 256 lanes 22.2 us,
-    // 1024 lanes 43.7) and enough for each lane, less where it saves the join (1 x 32000 bf16 256 lanes 5.0, 1024 lanes 4.4;
-    // 4 x 131072 in eight parts 12.5 / 13.1); two vectors in flight instead of four in short rows (8192 x 5000 bf16 24.7 / 26.1;
-    // 3475 x 9296 binary16, 20 alternatives, 38.3 / 44.3)
-    const bool wide = a.rows * p.splits <= 256 && p.chunk >= (p.splits == 1 ? 2048 : 4096), uncached = a.rows * a.vocab * (kind == kF32 ? 4 : 2) >= kUncached;
+    static_assert(kRowVec == kVec, "");
+    const LogProbsShape shape = logprobs_shape(a.rows, a.vocab, a.top, kind == kF32 ? 4 : 2);
+    const LogProbsArgs p{a, shape.splits, shape.chunk};
     return dispatch_kind(kind, [&](auto K) {
         constexpr int KIND = decltype(K)::value;
         auto run = [&](auto L, auto U, auto N) { return dispatch_flag(a.top > 0, [&](auto T) { return dispatch_flag(a.entropy, [&](auto E) {
@@ -607,10 +585,10 @@ int launch_logprobs(const LogProbs& a, int kind, void* stream)
                                dim3(grid_of(a.rows * p.splits)), dim3(LANES), 0, stream, p);
         }); }); };
         using std::integral_constant;
-        const int err = wide ? run(integral_constant<int, 1024>{}, integral_constant<int, 4>{}, std::false_type{})
-                      : p.chunk < (a.top ? 2048 : 1024) ? run(integral_constant<int, 256>{}, integral_constant<int, 2>{}, std::false_type{})
-                      : uncached ? run(integral_constant<int, 256>{}, integral_constant<int, 4>{}, std::true_type{})
-                                 : run(integral_constant<int, 256>{}, integral_constant<int, 4>{}, std::false_type{});
+        const int err = shape.lanes == 1024 ? run(integral_constant<int, 1024>{}, integral_constant<int, 4>{}, std::false_type{})
+                      : shape.flight == 2   ? run(integral_constant<int, 256>{}, integral_constant<int, 2>{}, std::false_type{})
+                      : shape.uncached      ? run(integral_constant<int, 256>{}, integral_constant<int, 4>{}, std::true_type{})
+                                            : run(integral_constant<int, 256>{}, integral_constant<int, 4>{}, std::false_type{});
         if (err || p.splits == 1) return err;
         return dispatch_flag(a.top > 0, [&](auto T) {
             return launch_args(join_kernel<KIND, decltype(T)::value>, dim3(grid_of(a.rows)), dim3(kJoinLanes), 0, stream, p);
@@ -620,13 +598,10 @@ int launch_logprobs(const LogProbs& a, int kind, void* stream)
 
 int launch_logprobs_backward(const LogProbsBackward& a, int kind, void* stream)
 {
-    const unsigned vecs = (unsigned)(((size_t)a.vocab + kVec - 1) / kVec);
-    // 32 bytes for each lane (4096 x 65536 bf16: one vector 192 us, two 165, four 176; 2000 x 50001 f32: one 141, two 156, four 169)
-    LogProbsBackwardArgs p{a, (kind == kF32 ? 1u : 2u) * kGradLanes, 0};
-    p.chunks = (vecs + p.chunk - 1) / p.chunk;
-    const bool unkept = a.rows * a.vocab * (kind == kF32 ? 4 : 2) >= kUnkept;
+    const GradientShape shape = gradient_shape(a.rows, a.vocab, kind == kF32 ? 4 : 2);
+    const LogProbsBackwardArgs p{a, shape.chunk, shape.chunks};
     return dispatch_kind(kind, [&](auto K) { return dispatch_tail(a.vocab, [&](auto T) { return dispatch_flag(a.dentropy, [&](auto E) {
-        return dispatch_flag(unkept, [&](auto N) {
+        return dispatch_flag(shape.unkept, [&](auto N) {
             return launch_args(logprobs_backward_kernel<decltype(K)::value, decltype(T)::value, decltype(E)::value, decltype(N)::value>,
                                dim3(grid_of(a.rows * p.chunks)), dim3(kGradLanes), 0, stream, p);
         });
