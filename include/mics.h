@@ -46,9 +46,10 @@
  *     itself (an earlier, unrelated HIP error of the thread is neither reported
  *     nor cleared); every entry point issues a single launch, except the
  *     coalesced ones, which issue one per 48 to 96 tensors, backward passes
- *     that sum over rows (two, or three with very long rows) and log
- *     probabilities of few long rows (two): these may have enqueued earlier
- *     launches when a later one fails.
+ *     that sum over rows (one with few rows or none, else two, and one more
+ *     with rows of more than 8192 columns) and log probabilities of few long
+ *     rows (two): these may have enqueued earlier launches when a later one
+ *     fails.
  *   - Return value: MICS_OK or a negative MICS_ERR_*; mics_last_error() gives
  *     the text for the calling thread's most recent failure.
  *   - bf16 values travel as uint16_t bit patterns (upper half of a binary32).

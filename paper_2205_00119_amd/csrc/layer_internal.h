@@ -63,7 +63,8 @@ struct DropoutPass {
     float* parts;                         // backward with dbias
 };
 
-// Column sums are formed in groups of rows: of three sums at most so many groups, of one twice as many.
+// Column sums are formed in groups of rows: of the norms' two or three sums at most so many groups, of the dropout's one twice as
+// many.
 constexpr size_t kMostParts = 256;
 // Rows of more elements than this do not stay in a workgroup's registers in the backward pass.
 constexpr size_t kTiledCols = 8192;
@@ -73,10 +74,12 @@ constexpr size_t kMostCols = size_t{1} << 24;
 
 // `fused`: bias, residual, dropout, sum; otherwise the norm alone.
 int launch_norm(const NormForward& a, int kind, bool fused, void* stream);
-// dx and the sums by group of rows, then the sums: two launches, three of rows longer than kTiledCols.  grads: dweight,
-// dnorm_bias and, with `fused`, dbias, of kind `grad`, each may be NULL.
+// dx and the sums by group of rows, then the sums: two launches.  One where a workgroup takes all rows (few rows of at most
+// kTiledCols) and without rows; rows longer than kTiledCols take one more, in front.  grads: dweight, dnorm_bias and, with
+// `fused`, dbias, of kind `grad`, each may be NULL.
 int launch_norm_backward(const NormBackward& a, int kind, bool fused, void* const* grads, int grad, void* stream);
 int launch_dropout(const DropoutPass& a, int kind, void* stream);
+// Two launches; one for few rows, for very long ones (one workgroup for each stripe of them) and without rows.
 int launch_dropout_backward(const DropoutPass& a, int kind, void* dbias, int grad, void* stream);
 
 struct LogProbs {

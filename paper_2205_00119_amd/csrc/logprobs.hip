@@ -4,9 +4,9 @@
 //     log p_j = x_j - m - log Z,    entropy = log Z - T / Z,
 // so one pass that keeps (m, Z, T) and rescales them when m grows reads every logit once.  Z and T of two parts join as
 //     Z = Z1 e^(m1-m) + Z2 e^(m2-m),    T = sum of e^(mi-m) (Ti + (mi-m) Zi).
-// Bound by HBM bandwidth with many rows, by latency with few.  Measured on one MI355X: 4096 x 65536 bf16 with entropy 82.0 us =
-// 6.5 TB/s; 500 x 50001 f32 with 5 alternatives 22.4 us = 4.5 TB/s; 4 x 131072 bf16 with 8 12.5 us, two launches; the gradient of
-// 4096 x 65536 165.7 us = 6.5 TB/s read and written.
+// Bound by HBM bandwidth with many rows, by latency with few.  Measured on one MI355X: 4096 x 65536 bf16 with entropy 83.3 us =
+// 6.45 TB/s; 500 x 50001 f32 with 5 alternatives 22.3 us = 4.5 TB/s; 4 x 131072 bf16 with 8 12.4 us, two launches; the gradient of
+// 4096 x 65536 165.8 us = 6.5 TB/s read and written.
 #include "rows.h"
 
 #include <algorithm>
@@ -205,8 +205,8 @@ template <int LANES> __device__ __forceinline__ float reached_by(LogProbsLds<LAN
 }
 
 // The first `top` of the n candidates in order into lds.best, n the same in all lanes.  Many candidates are thinned out
-// first, by the threshold of their own runs (300 x 100000 bf16, half of them masked, 50 alternatives, with 256 lanes a row: some
-// 1200 candidates, 584 us without, 64 so).
+// first, by the threshold of their own runs (300 x 100000 bf16, half of them masked, 50 alternatives: some 1150 candidates, 259 us
+// without, 47.7 so).
 template <int LANES> __device__ __forceinline__ void rank_candidates(LogProbsLds<LANES, true>& lds, int n, int top)
 {
     if (n > 3 * 64) {
@@ -360,8 +360,10 @@ __device__ __forceinline__ void write_best(const LogProbs& a, size_t row, int k,
 
 // One pass: U vectors of every lane are worked on while the next U are loaded.  TOP: the first U tell a threshold, and what
 // reaches it is kept as a candidate on the way.
-// Four wavefronts for each unit of a compute unit where that spills nothing (2048 x 32768 bf16, 5 alternatives: three 42.0 us, four
-// 38.9; of 32-bit logits, which spill, 500 x 50001 22.2 / 25.8).
+// Four wavefronts for each unit of a compute unit, which takes 128 registers, where that spills little: two registers of 16-bit logits
+// (2048 x 32768 bf16, 5 alternatives: three wavefronts 42.3 us, four 38.8).  32-bit ones keep their 172 (500 x 50001, 5
+// alternatives: 22.3 us, four 25.9).  1024 lanes leave no choice: two registers spill, of 32-bit logits 12 to 17 (1 x 32000 f32, 5
+// alternatives, 10.9 us).
 template <int KIND, int LANES, int U, bool TOP, bool ENTROPY, bool NT>
 __global__ __launch_bounds__(LANES, LANES == 256 && U == 4 && TOP && KIND != kF32 ? 4 : 1) void logprobs_kernel(LogProbsArgs p)
 {

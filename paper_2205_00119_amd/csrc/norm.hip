@@ -1,12 +1,14 @@
 // Layer norm, alone and behind bias, dropout and residual in one pass, forward and backward.
 //
-// Every byte is read once and written once: a row stays in the registers of the lanes that read it, from the load to the
-// last store.  Bound by HBM bandwidth at large sizes, by launches and reductions at small ones.  Workgroups stay on their
-// compute unit and go from row to row; the loads of the next row are in flight while one is worked on.
+// Rows that fit a workgroup's registers (forward up to 16384 columns, backward up to 8192) are read once and written once: a row stays
+// with the lanes that read it, from the load to the last store.  Longer ones are read three times forward and twice backward,
+// from the caches where these hold them.  Bound by HBM bandwidth at large sizes, by launches and reductions at small ones.
+// Workgroups stay on their compute unit and go from row to row; the loads of the next row are in flight while one is worked on.
 //
 // Measured on one MI355X, bf16, three sets of buffers in turn: forward 8192 x 8192 49.2 us = 5.46 TB/s (HBM traffic equal to the
 // algorithmic bytes), with bias, dropout and residual 4096 x 5120 36.1 us = 4.65 TB/s; backward 4096 x 4096 25.4 us, 20 of them in
-// the first kernel (5.0 TB/s), with all there is 4096 x 8192 74.0 us = 4.5 TB/s, 67 in the first.  Results are left to the caches
+// the first kernel (5.0 TB/s), with all there is 4096 x 8192 74.1 us = 4.5 TB/s, 67 in the first.  Longer rows: forward 2048 x 16400
+// 43.8 us = 3.1 TB/s, backward with all there is 4096 x 12288 150 us = 3.4 TB/s of what has to be moved.  Results are left to the caches
 // for whoever reads them next: stored past them the forward pass is up to 20 % shorter by itself (4096 x 5120 28.5 us), but
 // with the kernels that read y and sum behind it 4 % longer (69.2 / 71.9; 4096 x 4096 55.7 / 59.9).
 #include "rows.h"
@@ -475,7 +477,9 @@ int launch_norm(const NormForward& given, int kind, bool fused, void* stream)
             }); });
         };
         // One vector in each lane for a row of one wavefront, two for longer ones (8192 x 8192 bf16: one 54.1 us, two 49.4); with
-        // dropout one, whose parameters and two rows fit the registers (4096 x 5120: one 36.1 us, two 68.1), up to 8192 columns.
+        // dropout one, whose parameters and two rows fit the registers (4096 x 5120: one 36.1 us, two 68.1), up to 8192 columns.  Up to
+        // 16384 two, whose parameters are read again for every row (4096 x 12288 98.9 us = 4.1 TB/s; 2048 x 12285 f32, whose rest spills
+        // five registers, 101.5).
         if (waves_of(vecs, 1) <= 1) return with(Int<1>{}, Int<3>{}, Int<256>{}, std::true_type{});
         if constexpr (FUSED) {
             if (waves_of(vecs, 1) <= kMostWaves) return with(Int<1>{}, Int<2>{}, Int<1024>{}, std::true_type{});
@@ -518,8 +522,11 @@ int launch_norm_backward(const NormBackward& given, int kind, bool fused, void* 
                 });
             };
             // One vector in each lane, two rows in registers (4096 x 8192 bf16 with all there is: two 74 us, three 94, which
-            // spill).  Longer rows in tiles of 8192 columns (4096 x 12288 bf16: tiles 105 us, two vectors in each lane 93, with
-            // all there is 151 / 273; 1024 x 12288 f32 59 / 70).
+            // spill).  Two spill as well where there is most to hold: behind dropout with a rest 6 to 12 registers of 128 (f32 10
+            // to 33), f32 with dsum 9 on whole vectors, tiles with dsum 2 to 22.  4096 x 5120 f32 without dsum 70.6 us and with it
+            // 92.2, 4096 x 5121 133.3; bf16 4096 x 5121 without 49.5 and with 76.9.  Longer rows in tiles of 8192 columns: two vectors
+            // in each lane are faster for the norm alone (4096 x 12288 bf16: tiles 105 us, so 93) and much slower with all there
+            // is (150 / 273; 1024 x 12288 f32 59 / 70), and one way serves all.
             if (a.cols > kTiledCols) {
                 if (int e = launch_args(row_sums_kernel<KIND>, dim3(grid_of(a.rows)), dim3(1024), 0, stream, p)) return e;
                 return with(Int<1>{}, Int<2>{}, std::true_type{});
