@@ -19,8 +19,10 @@
  *
  * and, in the last part of this header, operators that the rank runs on the
  * gathered parameters before there is a gradient to reduce: layer norm,
- * dropout with bias and residual, both in one pass, and token log
- * probabilities, each forward and backward.
+ * dropout with bias and residual, both in one pass, token log
+ * probabilities, the linear layer with bias, activation and residual in its
+ * epilogue, and activations with their 8-bit checkpoints, each forward and
+ * backward.
  *
  * Notation (paper Section 3.1): k = devices per node, p = devices holding one
  * model replica (partition group size), s = micro-steps.  r = size of a
@@ -47,9 +49,9 @@
  *     nor cleared); every entry point issues a single launch, except the
  *     coalesced ones, which issue one per 48 to 96 tensors, backward passes
  *     that sum over rows (one with few rows or none, else two, and one more
- *     with rows of more than 8192 columns) and log probabilities of few long
- *     rows (two): these may have enqueued earlier launches when a later one
- *     fails.
+ *     with rows of more than 8192 columns), log probabilities of few long
+ *     rows (two) and products of few tiles (two): these may have enqueued
+ *     earlier launches when a later one fails.
  *   - Return value: MICS_OK or a negative MICS_ERR_*; mics_last_error() gives
  *     the text for the calling thread's most recent failure.
  *   - bf16 values travel as uint16_t bit patterns (upper half of a binary32).
@@ -429,6 +431,99 @@ int mics_token_logprobs_backward(void* dlogits, const void* logits, const int64_
                                  const float* lse, const float* entropy, const float* dlogprob,
                                  const float* dentropy, size_t rows, size_t vocab,
                                  const size_t* strides, int dtype, void* stream);
+
+/*
+ * Activations:
+ *     RELU       z > 0 ? z : 0, slope z > 0 ? 1 : 0
+ *     GELU       z P(z), P the distribution function of the standard normal
+ *     GELU_TANH  z / (1 + exp(-2 sqrt(2/pi) (z + 0.044715 z^3)))
+ *     SILU       z / (1 + exp(-z))
+ * NaN stays NaN (RELU too); z = -inf gives NaN as 0 * inf does, but 0 for RELU.
+ */
+#define MICS_ACT_NONE      0
+#define MICS_ACT_RELU      1
+#define MICS_ACT_GELU      2
+#define MICS_ACT_GELU_TANH 3
+#define MICS_ACT_SILU      4
+
+/*
+ * Activation checkpoints in 8 bits.  A matrix z of `rows` rows of `cols` columns is kept as `codes` (int8, a row stride of its
+ * own) and `scales` (fp32, packed): every row is cut into blocks of MICS_CHECKPOINT_BLOCK columns, the last one shorter, and
+ * scales[row * ceil(cols / 64) + b] belongs to block b.  In binary32, each operation rounded to nearest even, for every block
+ *     top = max(max |z|, 2^-100),   scale = top / 127,   code = rint(z * (127 / top)),
+ * and an element stands for code * scale: it is off by at most half a scale and the roundings.  A block that holds an
+ * infinity or NaN has the scale NaN and codes of 0: all of it stands for NaN.
+ * mics_checkpoint_scales: rows * ceil(cols / 64), the number of scales; 0 on bad arguments.
+ */
+#define MICS_CHECKPOINT_BLOCK 64
+size_t mics_checkpoint_scales(size_t rows, size_t cols);
+
+/*
+ *     z = x + bias,   y = act(z),   codes, scales = the checkpoint of z
+ *   strides         y, codes, x
+ *   bias            cols, may be NULL (0)
+ *   y               may be NULL: the checkpoint alone
+ *   codes, scales   may be NULL, both or neither
+ */
+int mics_activation(void* y, int8_t* codes, float* scales, const void* x, const void* bias, size_t rows, size_t cols,
+                    const size_t* strides, int act, int dtype, int param_dtype, void* stream);
+
+/*
+ *     y = act(z), z what the checkpoint stands for (act = MICS_ACT_NONE: z itself)
+ *   strides   y, codes
+ */
+int mics_checkpoint_read(void* y, const int8_t* codes, const float* scales, size_t rows, size_t cols, const size_t* strides,
+                         int act, int dtype, void* stream);
+
+/*
+ *     dx = dy * act'(z),   dbias[c] = sum over the rows of dx[., c], before it is rounded
+ * z is either the matrix `z` or what the checkpoint stands for: the other one is NULL.
+ *   strides     dx, dy, z, codes
+ *   dx          may be NULL: dbias alone
+ *   dbias       cols, may be NULL; then no workspace is needed
+ *   workspace   mics_column_workspace_bytes(rows, cols)
+ */
+int mics_activation_backward(void* dx, void* dbias, const void* dy, const void* z, const int8_t* codes, const float* scales,
+                             size_t rows, size_t cols, const size_t* strides, int act, int dtype, int grad_dtype,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The linear layer.  x: rows rows of in_features, weight: out_features rows of in_features, both of `dtype`;
+ *     z = x weight^T + bias,   out = residual + act(z)
+ * and for the backward pass pre = z in `dtype`, or codes, scales = its checkpoint.  The act, the residual and the checkpoint take
+ * z before it is rounded.  Products of 16-bit elements are exact and summed in binary32 in an order that depends on sizes,
+ * strides and alignment alone.
+ *   strides          out, pre, codes, x, weight, residual
+ *   pre              may be NULL
+ *   codes, scales    of out_features columns; may be NULL, both or neither
+ *   bias             out_features of param_dtype, may be NULL (0)
+ *   residual         may be NULL (0), may be out
+ *   workspace        mics_linear_workspace_bytes(rows, in_features, out_features), at most 64 MiB and 0 for large products:
+ *                    few tiles are shared by several workgroups, whose sums a second launch joins
+ * out may not take the place of x or weight.  1 <= in_features, out_features <= 2^24.
+ */
+size_t mics_linear_workspace_bytes(size_t rows, size_t in_features, size_t out_features);
+int mics_linear(void* out, void* pre, int8_t* codes, float* scales, const void* x, const void* weight, const void* bias,
+                const void* residual, size_t rows, size_t in_features, size_t out_features, const size_t* strides, int act,
+                int dtype, int param_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ *     dx = dz weight + dsum
+ * with dz = rows rows of out_features, the gradient of z (mics_activation_backward forms it, with the bias's gradient).
+ *   strides   dx, dz, weight, dsum
+ *   dsum      gradient that reaches x by other ways, may be NULL (0), may be dx
+ */
+int mics_linear_backward_input(void* dx, const void* dz, const void* weight, const void* dsum, size_t rows,
+                               size_t in_features, size_t out_features, const size_t* strides, int dtype,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ *     dweight = dz^T x,  out_features rows of in_features; zeros without rows
+ *   strides   dweight, dz, x
+ */
+int mics_linear_backward_weight(void* dweight, const void* dz, const void* x, size_t rows, size_t in_features,
+                                size_t out_features, const size_t* strides, int dtype, int grad_dtype, void* workspace,
+                                size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -33,8 +33,12 @@ EXPORTS = (
     "mics_bias_dropout_add", "mics_bias_dropout_add_backward", "mics_layer_norm", "mics_layer_norm_backward",
     "mics_dropout_add_layer_norm", "mics_dropout_add_layer_norm_backward",
     "mics_token_logprobs", "mics_token_logprobs_backward",
+    "mics_checkpoint_scales", "mics_linear_workspace_bytes", "mics_activation", "mics_checkpoint_read",
+    "mics_activation_backward", "mics_linear", "mics_linear_backward_input", "mics_linear_backward_weight",
 )
 MICS_MAX_TOP = 64
+MICS_CHECKPOINT_BLOCK = 64
+MICS_ACT_NONE, MICS_ACT_RELU, MICS_ACT_GELU, MICS_ACT_GELU_TANH, MICS_ACT_SILU = range(5)
 MICS_DTYPE_BF16, MICS_DTYPE_F16, MICS_DTYPE_F32 = 0, 1, 2
 
 
@@ -129,7 +133,18 @@ lib.mics_token_logprobs.argtypes = [_vp] * 7 + [_sz, _sz, _sz, _i, _i, _vp, _sz,
 lib.mics_token_logprobs_backward.argtypes = [_vp] * 7 + [_sz, _sz, _vp, _i, _vp]
 _LAYER_CALLS = ("bias_dropout_add", "bias_dropout_add_backward", "layer_norm", "layer_norm_backward", "dropout_add_layer_norm",
                 "dropout_add_layer_norm_backward", "token_logprobs", "token_logprobs_backward")
-for _name in _LAYER_CALLS:
+lib.mics_checkpoint_scales.argtypes = [_sz, _sz]
+lib.mics_checkpoint_scales.restype = _sz
+lib.mics_linear_workspace_bytes.argtypes = [_sz, _sz, _sz]
+lib.mics_linear_workspace_bytes.restype = _sz
+lib.mics_activation.argtypes = [_vp] * 5 + [_sz, _sz, _vp, _i, _i, _i, _vp]
+lib.mics_checkpoint_read.argtypes = [_vp] * 3 + [_sz, _sz, _vp, _i, _i, _vp]
+lib.mics_activation_backward.argtypes = [_vp] * 6 + [_sz, _sz, _vp, _i, _i, _i, _vp, _sz, _vp]
+lib.mics_linear.argtypes = [_vp] * 8 + [_sz, _sz, _sz, _vp, _i, _i, _i, _vp, _sz, _vp]
+lib.mics_linear_backward_input.argtypes = [_vp] * 4 + [_sz, _sz, _sz, _vp, _i, _vp, _sz, _vp]
+lib.mics_linear_backward_weight.argtypes = [_vp] * 3 + [_sz, _sz, _sz, _vp, _i, _i, _vp, _sz, _vp]
+_LINEAR_CALLS = ("activation", "checkpoint_read", "activation_backward", "linear", "linear_backward_input", "linear_backward_weight")
+for _name in _LAYER_CALLS + _LINEAR_CALLS:
     getattr(lib, "mics_" + _name).restype = _i
 
 
@@ -176,6 +191,7 @@ _marshal.bind(tuple(ctypes.cast(getattr(lib, "mics_" + name), _vp).value for nam
     "adam_shard_typed", "replica_average_adam_shard", "replica_average_adam_shard_typed")),
     _device, _raw_stream)
 _marshal.bind_layer(tuple(ctypes.cast(getattr(lib, "mics_" + name), _vp).value for name in _LAYER_CALLS))
+_marshal.bind_linear(tuple(ctypes.cast(getattr(lib, "mics_" + name), _vp).value for name in _LINEAR_CALLS))
 _marshal.bind_segment(mics_segment)
 
 
@@ -465,3 +481,81 @@ def mics_token_logprobs_backward(dlogits, logits, targets, lse, entropy, dlogpro
     _check(lib.mics_token_logprobs_backward(_matrix(dlogits, st, 0), _matrix(logits, st, 1), _dev_ptr(targets), _dev_ptr(lse),
                                             _dev_ptr(entropy), _dev_ptr(dlogprob), _dev_ptr(dentropy), rows, vocab, st, dtype,
                                             _stream(stream)))
+
+
+# The linear layer and activations with their 8-bit checkpoints; codes are int8 tensors, scales packed float32.
+
+def mics_checkpoint_scales(rows: int, cols: int) -> int:
+    """Scales of a checkpoint: one for every 64 columns of a row."""
+    return lib.mics_checkpoint_scales(rows, cols)
+
+
+def mics_linear_workspace_bytes(rows: int, in_features: int, out_features: int) -> int:
+    """Workspace of the linear layer and of the gradients of its input and weight, at most 64 MiB."""
+    return lib.mics_linear_workspace_bytes(rows, in_features, out_features)
+
+
+def mics_activation(y, codes, scales, x, bias, rows: int, cols: int, *, act: int, dtype: int, param_dtype: int, strides=None,
+                    stream=None) -> None:
+    """y = act(x + bias) and the 8-bit checkpoint of x + bias; strides: y, codes, x."""
+    if _done(_marshal.activation(y, codes, scales, x, bias, rows, cols, strides, act, dtype, param_dtype, stream)):
+        return
+    st = _strides(strides, 3)
+    _check(lib.mics_activation(_matrix(y, st, 0), _matrix(codes, st, 1), _dev_ptr(scales), _matrix(x, st, 2), _dev_ptr(bias), rows, cols,
+                               st, act, dtype, param_dtype, _stream(stream)))
+
+
+def mics_checkpoint_read(y, codes, scales, rows: int, cols: int, *, act: int, dtype: int, strides=None, stream=None) -> None:
+    """y = act(what the checkpoint stands for); strides: y, codes."""
+    if _done(_marshal.checkpoint_read(y, codes, scales, rows, cols, strides, act, dtype, stream)):
+        return
+    st = _strides(strides, 2)
+    _check(lib.mics_checkpoint_read(_matrix(y, st, 0), _matrix(codes, st, 1), _dev_ptr(scales), rows, cols, st, act, dtype,
+                                    _stream(stream)))
+
+
+def mics_activation_backward(dx, dbias, dy, z, codes, scales, rows: int, cols: int, *, act: int, dtype: int, grad_dtype: int,
+                             workspace=None, workspace_bytes: int = 0, strides=None, stream=None) -> None:
+    """dx = dy * act'(z) and its column sums, z a matrix or a checkpoint; strides: dx, dy, z, codes."""
+    if _done(_marshal.activation_backward(dx, dbias, dy, z, codes, scales, rows, cols, strides, act, dtype, grad_dtype, workspace,
+                                          workspace_bytes, stream)):
+        return
+    st = _strides(strides, 4)
+    _check(lib.mics_activation_backward(_matrix(dx, st, 0), _dev_ptr(dbias), _matrix(dy, st, 1), _matrix(z, st, 2), _matrix(codes, st, 3),
+                                        _dev_ptr(scales), rows, cols, st, act, dtype, grad_dtype, _dev_ptr(workspace), workspace_bytes,
+                                        _stream(stream)))
+
+
+def mics_linear(out, pre, codes, scales, x, weight, bias, residual, rows: int, in_features: int, out_features: int, *, act: int,
+                dtype: int, param_dtype: int, workspace=None, workspace_bytes: int = 0, strides=None, stream=None) -> None:
+    """out = residual + act(z), z = x weight^T + bias, and z as `pre` or as a checkpoint; strides: out, pre, codes, x, weight,
+    residual."""
+    if _done(_marshal.linear(out, pre, codes, scales, x, weight, bias, residual, rows, in_features, out_features, strides, act, dtype,
+                             param_dtype, workspace, workspace_bytes, stream)):
+        return
+    st = _strides(strides, 6)
+    _check(lib.mics_linear(_matrix(out, st, 0), _matrix(pre, st, 1), _matrix(codes, st, 2), _dev_ptr(scales), _matrix(x, st, 3),
+                           _matrix(weight, st, 4), _dev_ptr(bias), _matrix(residual, st, 5), rows, in_features, out_features, st, act,
+                           dtype, param_dtype, _dev_ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def mics_linear_backward_input(dx, dz, weight, dsum, rows: int, in_features: int, out_features: int, *, dtype: int, workspace=None,
+                               workspace_bytes: int = 0, strides=None, stream=None) -> None:
+    """dx = dz weight + dsum; strides: dx, dz, weight, dsum."""
+    if _done(_marshal.linear_backward_input(dx, dz, weight, dsum, rows, in_features, out_features, strides, dtype, workspace,
+                                            workspace_bytes, stream)):
+        return
+    st = _strides(strides, 4)
+    _check(lib.mics_linear_backward_input(_matrix(dx, st, 0), _matrix(dz, st, 1), _matrix(weight, st, 2), _matrix(dsum, st, 3), rows,
+                                          in_features, out_features, st, dtype, _dev_ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def mics_linear_backward_weight(dweight, dz, x, rows: int, in_features: int, out_features: int, *, dtype: int, grad_dtype: int,
+                                workspace=None, workspace_bytes: int = 0, strides=None, stream=None) -> None:
+    """dweight = dz^T x; strides: dweight, dz, x."""
+    if _done(_marshal.linear_backward_weight(dweight, dz, x, rows, in_features, out_features, strides, dtype, grad_dtype, workspace,
+                                             workspace_bytes, stream)):
+        return
+    st = _strides(strides, 3)
+    _check(lib.mics_linear_backward_weight(_matrix(dweight, st, 0), _matrix(dz, st, 1), _matrix(x, st, 2), rows, in_features,
+                                           out_features, st, dtype, grad_dtype, _dev_ptr(workspace), workspace_bytes, _stream(stream)))

@@ -6,7 +6,8 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(HERE, "libmics.so")
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("api.cpp", "layer_api.cpp", "kernels.hip", "norm.hip", "dropout.hip", "logprobs.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in (
+    "api.cpp", "layer_api.cpp", "linear_api.cpp", "kernels.hip", "norm.hip", "dropout.hip", "logprobs.hip", "activation.hip", "linear.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -21,7 +22,7 @@ FLAGS = [
 
 def build(extra_flags=(), out: str = LIB, verbose: bool = False) -> str:
     tmp = out + f".tmp{os.getpid()}"
-    cmd = [HIPCC, *FLAGS, *extra_flags, "-parallel-jobs=4", "-o", tmp, *SOURCES]
+    cmd = [HIPCC, *FLAGS, *extra_flags, "-parallel-jobs=8", "-o", tmp, *SOURCES]
     res = subprocess.run(cmd, capture_output=True, text=True)
     noise = "is not a recognized feature for this target"
     log = "\n".join(l for l in (res.stdout + res.stderr).splitlines() if noise not in l)

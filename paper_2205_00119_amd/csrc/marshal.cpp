@@ -8,7 +8,7 @@
 // buffers, 8 MB 5.7 / 4.9, of 76 segments 8.0 / 6.1, Adam 5.9 / 5.1; the launch itself is 2.5 to 4 of them.
 // Whatever they do not know they leave alone and return None; the entry point then goes through ctypes.
 //
-// No state but what bind(), bind_layer() and bind_segment() set at import.  Everything is called with the GIL held, which is given up
+// No state but what bind(), bind_layer(), bind_linear() and bind_segment() set at import.  Everything is called with the GIL held, which is given up
 // while the library works; nothing outlives the call.
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -199,6 +199,16 @@ struct {
     decltype(&mics_token_logprobs_backward) token_logprobs_backward;
 } layer;
 constexpr Py_ssize_t kLayerEntries = sizeof layer / sizeof(void*);
+// The entry points that bind_linear() sets.
+struct {
+    decltype(&mics_activation) activation;
+    decltype(&mics_checkpoint_read) checkpoint_read;
+    decltype(&mics_activation_backward) activation_backward;
+    decltype(&mics_linear) linear;
+    decltype(&mics_linear_backward_input) linear_backward_input;
+    decltype(&mics_linear_backward_weight) linear_backward_weight;
+} products;
+constexpr Py_ssize_t kProductEntries = sizeof products / sizeof(void*);
 PyObject *device_of_thread, *raw_stream, *segment_type;
 PyObject *stream_attr, *item_attr;                 // "cuda_stream", "_type_"
 
@@ -225,21 +235,24 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n)
     Py_RETURN_NONE;
 }
 
-// bind_layer(addresses in the order above)
-PyObject* bind_layer(PyObject*, PyObject* entries)
+// Entry points in the order of a table of `count` of them.
+PyObject* bind_table(PyObject* entries, void* table, Py_ssize_t count)
 {
-    if (!PyTuple_CheckExact(entries) || PyTuple_GET_SIZE(entries) != kLayerEntries) {
+    if (!PyTuple_CheckExact(entries) || PyTuple_GET_SIZE(entries) != count) {
         PyErr_SetString(PyExc_TypeError, "expected a tuple of addresses");
         return nullptr;
     }
-    void* at[kLayerEntries];
-    for (Py_ssize_t i = 0; i < kLayerEntries; ++i) {
+    void* at[kLayerEntries > kProductEntries ? kLayerEntries : kProductEntries];
+    for (Py_ssize_t i = 0; i < count; ++i) {
         at[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(entries, i));
         if (!at[i] && PyErr_Occurred()) return nullptr;
     }
-    std::memcpy((void*)&layer, at, sizeof at);
+    std::memcpy(table, at, (size_t)count * sizeof *at);
     Py_RETURN_NONE;
 }
+// bind_layer(addresses in the order above), bind_linear(addresses in the order above)
+PyObject* bind_layer(PyObject*, PyObject* entries) { return bind_table(entries, (void*)&layer, kLayerEntries); }
+PyObject* bind_linear(PyObject*, PyObject* entries) { return bind_table(entries, (void*)&products, kProductEntries); }
 
 // bind_segment(mics_segment, the ctypes structure)
 PyObject* bind_segment(PyObject*, PyObject* type)
@@ -383,7 +396,7 @@ class Call {
     int entries = 0, n_segments = 0;
 
   private:
-    static constexpr int kMaxSegments = 128, kMaxMatrices = 5;
+    static constexpr int kMaxSegments = 128, kMaxMatrices = 6;
     PyObject* const* a;
     bool plain, raised = false;
     void* pointers[MICS_MAX_GROUP];
@@ -750,6 +763,104 @@ MICS_CALL(token_logprobs_backward)
     });
 }
 
+// y codes scales x bias rows cols strides act dtype param_dtype stream
+MICS_CALL(activation)
+{
+    Call c(args, n, "pppppiiziiis");
+    const size_t* const st = c.strides(7, 3);
+    void* const y = c.matrix(0, at(st, 0));
+    int8_t* const codes = (int8_t*)c.matrix(1, at(st, 1));
+    float* const scales = (float*)c.ptr(2);
+    const void *const x = c.matrix(3, at(st, 2)), *const bias = c.ptr(4);
+    const size_t rows = c.size(5), cols = c.size(6);
+    const int act = c.num(8), dtype = c.num(9), param = c.num(10);
+    void* const s = c.stream(11);
+    return c.run([&] { return products.activation(y, codes, scales, x, bias, rows, cols, st, act, dtype, param, s); });
+}
+
+// y codes scales rows cols strides act dtype stream
+MICS_CALL(checkpoint_read)
+{
+    Call c(args, n, "pppiiziis");
+    const size_t* const st = c.strides(5, 2);
+    void* const y = c.matrix(0, at(st, 0));
+    const int8_t* const codes = (const int8_t*)c.matrix(1, at(st, 1));
+    const float* const scales = (const float*)c.ptr(2);
+    const size_t rows = c.size(3), cols = c.size(4);
+    const int act = c.num(6), dtype = c.num(7);
+    void* const s = c.stream(8);
+    return c.run([&] { return products.checkpoint_read(y, codes, scales, rows, cols, st, act, dtype, s); });
+}
+
+// dx dbias dy z codes scales rows cols strides act dtype grad_dtype workspace workspace_bytes stream
+MICS_CALL(activation_backward)
+{
+    Call c(args, n, "ppppppiiziiipis");
+    const size_t* const st = c.strides(8, 4);
+    void *const dx = c.matrix(0, at(st, 0)), *const dbias = c.ptr(1);
+    const void *const dy = c.matrix(2, at(st, 1)), *const z = c.matrix(3, at(st, 2));
+    const int8_t* const codes = (const int8_t*)c.matrix(4, at(st, 3));
+    const float* const scales = (const float*)c.ptr(5);
+    const size_t rows = c.size(6), cols = c.size(7);
+    const int act = c.num(9), dtype = c.num(10), grad = c.num(11);
+    void* const work = c.ptr(12);
+    const size_t bytes = c.size(13);
+    void* const s = c.stream(14);
+    return c.run([&] {
+        return products.activation_backward(dx, dbias, dy, z, codes, scales, rows, cols, st, act, dtype, grad, work, bytes, s);
+    });
+}
+
+// out pre codes scales x weight bias residual rows in out strides act dtype param_dtype workspace workspace_bytes stream
+MICS_CALL(linear)
+{
+    Call c(args, n, "ppppppppiiiziiipis");
+    const size_t* const st = c.strides(11, 6);
+    void *const out = c.matrix(0, at(st, 0)), *const pre = c.matrix(1, at(st, 1));
+    int8_t* const codes = (int8_t*)c.matrix(2, at(st, 2));
+    float* const scales = (float*)c.ptr(3);
+    const void *const x = c.matrix(4, at(st, 3)), *const weight = c.matrix(5, at(st, 4)), *const bias = c.ptr(6);
+    const void* const residual = c.matrix(7, at(st, 5));
+    const size_t rows = c.size(8), in = c.size(9), outs = c.size(10);
+    const int act = c.num(12), dtype = c.num(13), param = c.num(14);
+    void* const work = c.ptr(15);
+    const size_t bytes = c.size(16);
+    void* const s = c.stream(17);
+    return c.run([&] {
+        return products.linear(out, pre, codes, scales, x, weight, bias, residual, rows, in, outs, st, act, dtype, param, work, bytes, s);
+    });
+}
+
+// dx dz weight dsum rows in out strides dtype workspace workspace_bytes stream
+MICS_CALL(linear_backward_input)
+{
+    Call c(args, n, "ppppiiizipis");
+    const size_t* const st = c.strides(7, 4);
+    void* const dx = c.matrix(0, at(st, 0));
+    const void *const dz = c.matrix(1, at(st, 1)), *const weight = c.matrix(2, at(st, 2)), *const dsum = c.matrix(3, at(st, 3));
+    const size_t rows = c.size(4), in = c.size(5), outs = c.size(6);
+    const int dtype = c.num(8);
+    void* const work = c.ptr(9);
+    const size_t bytes = c.size(10);
+    void* const s = c.stream(11);
+    return c.run([&] { return products.linear_backward_input(dx, dz, weight, dsum, rows, in, outs, st, dtype, work, bytes, s); });
+}
+
+// dweight dz x rows in out strides dtype grad_dtype workspace workspace_bytes stream
+MICS_CALL(linear_backward_weight)
+{
+    Call c(args, n, "pppiiiziipis");
+    const size_t* const st = c.strides(6, 3);
+    void* const dweight = c.matrix(0, at(st, 0));
+    const void *const dz = c.matrix(1, at(st, 1)), *const x = c.matrix(2, at(st, 2));
+    const size_t rows = c.size(3), in = c.size(4), outs = c.size(5);
+    const int dtype = c.num(7), grad = c.num(8);
+    void* const work = c.ptr(9);
+    const size_t bytes = c.size(10);
+    void* const s = c.stream(11);
+    return c.run([&] { return products.linear_backward_weight(dweight, dz, x, rows, in, outs, st, dtype, grad, work, bytes, s); });
+}
+
 #define MICS_METHOD(name) {#name, (PyCFunction)(void (*)())name, METH_FASTCALL, "A whole call; None if an argument is not plain."}
 
 PyMethodDef methods[] = {
@@ -765,6 +876,9 @@ PyMethodDef methods[] = {
     MICS_METHOD(bias_dropout_add), MICS_METHOD(bias_dropout_add_backward), MICS_METHOD(layer_norm),
     MICS_METHOD(layer_norm_backward), MICS_METHOD(dropout_add_layer_norm), MICS_METHOD(dropout_add_layer_norm_backward),
     MICS_METHOD(token_logprobs), MICS_METHOD(token_logprobs_backward),
+    {"bind_linear", bind_linear, METH_O, "Sets the entry points of the linear layer and of activations."},
+    MICS_METHOD(activation), MICS_METHOD(checkpoint_read), MICS_METHOD(activation_backward), MICS_METHOD(linear),
+    MICS_METHOD(linear_backward_input), MICS_METHOD(linear_backward_weight),
     {nullptr, nullptr, 0, nullptr},
 };
 
