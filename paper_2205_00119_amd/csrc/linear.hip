@@ -2,6 +2,7 @@
 #include "rows.h"
 
 #include <algorithm>
+#include <utility>
 
 #include "activation.h"
 #include "columns.h"
@@ -72,7 +73,40 @@ template <int KIND, bool TURNED, int ROWS, int LANES> struct Stage {
         const size_t at = TURNED ? (k0 + d) * m.stride + row0 + r : (row0 + r) * m.stride + k0 + d;
         return load_chunk<KIND>((const char*)m.data + at * kWidth<KIND>, right <= 0 || deep <= 0 ? 0 : TURNED ? right : deep);
     }
+    // Bytes from the tile's first element to chunk i.  Rows behind the last of `rows` from the tile's first on repeat it: what they
+    // give is not stored.
+    static __device__ __forceinline__ uint32_t offset(size_t stride, size_t rows, int i)
+    {
+        const uint32_t r = (uint32_t)min((size_t)row(i), rows - (TURNED ? kChunk<KIND> : 1)), d = depth(i), step = (uint32_t)stride;
+        return (TURNED ? d * step + r : r * step + d) * (uint32_t)kWidth<KIND>;
+    }
+    static __device__ __forceinline__ const char* first(const ConstRows& m, size_t row0, size_t k0)
+    {
+        return (const char*)m.data + (TURNED ? k0 * m.stride + row0 : row0 * m.stride + k0) * kWidth<KIND>;
+    }
+    static __device__ __forceinline__ size_t step(const ConstRows& m) { return TURNED ? m.stride * kRowBytes : kRowBytes; }
 };
+
+// 16 bytes for each lane from `base` + `offset` into the LDS from byte `to` + TO on, lane after lane.  It counts as a load in flight that
+// the compiler does not know of: landed() waits.  m0, which nothing else here uses, has to settle first.
+template <int TO> __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(base), "v"(offset), "s"(to), "i"(TO) : "memory", "scc");
+}
+// f(std::integral_constant<int, i>) for every i below N.
+template <int... I, typename F> __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F> __device__ __forceinline__ void each(F&& f) { each_of(std::make_integer_sequence<int, N>{}, f); }
+// All loads and LDS accesses of this wavefront are over, then all wavefronts are here.
+__device__ __forceinline__ void landed()
+{
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 // What a lane hands to the matrix instructions of 16 rows and half the k of a tile: chunk lane / 16 of row lane % 16.
 template <int KIND> struct Piece {
@@ -147,9 +181,15 @@ __device__ __forceinline__ size_t unit_of(size_t i, size_t units)
     return cache * each + min(cache, rest) + i / 8;
 }
 
+// Tiles of rows that are taken together, column by column: what runs at one time under one of the 8 L2 caches is then 8 x 4 tiles.
+// us, 4 / 8 / 16 rows of tiles / all: 4096 x 8192 x 32768 bf16 1673 / 1678 / 1904 / 1909, 8192 x 8192 x 8192 846 / 842 / 859 / 1167.
+constexpr size_t kBand = 8;
 constexpr int kStagePitch = 64 + 4;            // floats of a row of a wavefront's results in the LDS
 
-template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN>
+// One workgroup for a tile of BM x BN results, WM x WN wavefronts with 64 columns each.
+// DIRECT: whole chunks begin on 16 bytes, so tiles of k go straight into the LDS, two of them in flight; while a wavefront multiplies
+// one half of a tile it reads the next half.  Otherwise, and for a last part of a tile, through registers.
+template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN, bool DIRECT>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
 {
     constexpr int kLanes = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, kOut = TM < 4 ? TM : 4;
@@ -166,18 +206,35 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
     for (size_t i = blockIdx.x; i < g.units; i += gridDim.x) {
         const size_t unit = unit_of(i, g.units), tiles = g.tiles_m * g.tiles_n;
         const size_t split = unit / tiles, t = unit % tiles;
-        const size_t m0 = t % g.tiles_m * BM, n0 = t / g.tiles_m * BN;
-        const size_t first = split * g.depth * kDepth<KIND>;
+        const size_t band = t / (kBand * g.tiles_n), in_band = t % (kBand * g.tiles_n), high = min(kBand, g.tiles_m - band * kBand);
+        const size_t m0 = (band * kBand + in_band % high) * BM, n0 = in_band / high * BN;
+        size_t first = split * g.depth * kDepth<KIND>;
         const size_t last = min(p.k, first + g.depth * kDepth<KIND>);
         f32x4 acc[TM][TN] = {};
-        u32x4 ra[StageA::kCount], rb[StageB::kCount];
-        auto fetch = [&](size_t k0) {
+        typedef Piece<KIND> PieceA[TM];
+        typedef Piece<KIND> PieceB[TN];
+        auto read = [&](PieceA& pa, PieceB& pb, int at, int half) {
+            const Reader<KIND, AT, BM> a(tile + at * kTileBytes, wm * TM * 16);
+            const Reader<KIND, BT, BN> b(tile + at * kTileBytes + BM * kRowBytes, wn * TN * 16);
+            #pragma unroll
+            for (int n = 0; n < TN; ++n) pb[n] = b.read(n, half);
+            #pragma unroll
+            for (int m = 0; m < TM; ++m) pa[m] = a.read(m, half);
+        };
+        auto add = [&](const PieceA& pa, const PieceB& pb) {
+            #pragma unroll
+            for (int m = 0; m < TM; ++m) {
+                #pragma unroll
+                for (int n = 0; n < TN; ++n) multiply<KIND>(acc[m][n], pa[m], pb[n]);
+            }
+        };
+        auto fetch = [&](u32x4 (&ra)[StageA::kCount], u32x4 (&rb)[StageB::kCount], size_t k0) {
             #pragma unroll
             for (int c = 0; c < StageA::kCount; ++c) ra[c] = StageA::load(p.a, m0, k0, p.m, last, c);
             #pragma unroll
             for (int c = 0; c < StageB::kCount; ++c) rb[c] = StageB::load(p.b, n0, k0, p.n, last, c);
         };
-        auto put = [&](int at) {
+        auto put = [&](const u32x4 (&ra)[StageA::kCount], const u32x4 (&rb)[StageB::kCount], int at) {
             lds_char* const to = tile + at * kTileBytes + threadIdx.x * 16;
             #pragma unroll
             for (int c = 0; c < StageA::kCount; ++c) *(__attribute__((address_space(3))) u32x4*)(to + c * kLanes * 16) = ra[c];
@@ -185,30 +242,82 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
             for (int c = 0; c < StageB::kCount; ++c)
                 *(__attribute__((address_space(3))) u32x4*)(to + BM * kRowBytes + c * kLanes * 16) = rb[c];
         };
-        int at = 0;
-        if (first < last) {
-            fetch(first);
-            put(0);
-        }
-        for (size_t k0 = first; k0 < last; k0 += kDepth<KIND>, at ^= 1) {
-            __syncthreads();
-            const bool more = k0 + kDepth<KIND> < last;
-            if (more) fetch(k0 + kDepth<KIND>);
-            const Reader<KIND, AT, BM> a(tile + at * kTileBytes, wm * TM * 16);
-            const Reader<KIND, BT, BN> b(tile + at * kTileBytes + BM * kRowBytes, wn * TN * 16);
-            #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                Piece<KIND> pb[TN];
+        if constexpr (DIRECT) {
+            if (const size_t rest = last > first ? (last - first) % kDepth<KIND> : 0) {      // in front: a sum has no order
+                u32x4 ra[StageA::kCount], rb[StageB::kCount];
+                fetch(ra, rb, last - rest);
+                put(ra, rb, 0);
+                __syncthreads();
                 #pragma unroll
-                for (int n = 0; n < TN; ++n) pb[n] = b.read(n, half);
+                for (int half = 0; half < 2; ++half) {
+                    PieceA pa;
+                    PieceB pb;
+                    read(pa, pb, 0, half);
+                    add(pa, pb);
+                }
+                __syncthreads();
+            }
+            const size_t whole = last > first ? (last - first) / kDepth<KIND> : 0;
+            if (whole) {
+                uint32_t oa[StageA::kCount], ob[StageB::kCount];
                 #pragma unroll
-                for (int m = 0; m < TM; ++m) {
-                    const Piece<KIND> pa = a.read(m, half);
-                    #pragma unroll
-                    for (int n = 0; n < TN; ++n) multiply<KIND>(acc[m][n], pa, pb[n]);
+                for (int c = 0; c < StageA::kCount; ++c) oa[c] = StageA::offset(p.a.stride, p.m - m0, c);
+                #pragma unroll
+                for (int c = 0; c < StageB::kCount; ++c) ob[c] = StageB::offset(p.b.stride, p.n - n0, c);
+                const char *from_a = StageA::first(p.a, m0, first), *from_b = StageB::first(p.b, n0, first);
+                const size_t step_a = StageA::step(p.a), step_b = StageB::step(p.b);
+                const uint32_t place = (uint32_t)(uintptr_t)tile + wave * 1024;
+                auto load = [&](int at) {
+                    const uint32_t to = place + at * kTileBytes;
+                    each<StageA::kCount>([&](auto c) {
+                        load_to_lds<decltype(c)::value * kLanes * 16>(from_a, oa[decltype(c)::value], to);
+                    });
+                    each<StageB::kCount>([&](auto c) {
+                        load_to_lds<BM * kRowBytes + decltype(c)::value * kLanes * 16>(from_b, ob[decltype(c)::value], to);
+                    });
+                    from_a += step_a;
+                    from_b += step_b;
+                };
+                PieceA a0, a1;
+                PieceB b0, b1;
+                load(0);
+                if (whole > 1) load(1);
+                landed();
+                read(a0, b0, 0, 0);
+                int at = 0;
+                for (size_t k = whole; k; --k, at ^= 1) {
+                    read(a1, b1, at, 1);
+                    __builtin_amdgcn_sched_barrier(0);          // reads are issued before the products that they pass by
+                    add(a0, b0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    landed();
+                    if (k > 2) load(at);
+                    read(a0, b0, at ^ 1, 0);                    // behind the last tile: what nothing uses
+                    __builtin_amdgcn_sched_barrier(0);
+                    add(a1, b1);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            if (more) put(at ^ 1);
+        } else {
+            u32x4 ra[StageA::kCount], rb[StageB::kCount];
+            int at = 0;
+            if (first < last) {
+                fetch(ra, rb, first);
+                put(ra, rb, 0);
+            }
+            for (size_t k0 = first; k0 < last; k0 += kDepth<KIND>, at ^= 1) {
+                __syncthreads();
+                const bool more = k0 + kDepth<KIND> < last;
+                if (more) fetch(ra, rb, k0 + kDepth<KIND>);
+                #pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    PieceA pa;
+                    PieceB pb;
+                    read(pa, pb, at, half);
+                    add(pa, pb);
+                }
+                if (more) put(ra, rb, at ^ 1);
+            }
         }
         // A wavefront's results pass through the LDS into rows of 64 columns, eight to a lane.
         typedef __attribute__((address_space(3))) f32x4 lds_f4;
@@ -238,21 +347,37 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
     }
 }
 
+// Whether every chunk of an operand lies on 16 bytes and a tile's chunks within 32 bits of its first.
+bool direct(const ConstRows& m, bool turned, size_t rows, size_t width, size_t tile)
+{
+    return (uintptr_t)m.data % 16 == 0 && m.stride * width % 16 == 0 && (!turned || rows * width % 16 == 0)
+        && m.stride < (size_t{1} << 31) / width / std::max<size_t>(tile, kRowBytes);
+}
+
+template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN, bool DIRECT> int launch_tiles(ProductArgs g, void* stream)
+{
+    g.tiles_m = ceil_div(g.p.m, BM);
+    g.tiles_n = ceil_div(g.p.n, BN);
+    g.units = g.tiles_m * g.tiles_n * g.splits;
+    return launch_args(product_kernel<KIND, AT, BT, BM, BN, WM, WN, DIRECT>, dim3(grid_of(g.units)), dim3(64 * WM * WN), 0, stream, g);
+}
+
 }  // namespace
 
 int launch_product(const Product& p, int kind, void* stream)
 {
-    constexpr int BM = 128, BN = 128;
-    ProductArgs g{p, ceil_div(p.m, BM), ceil_div(p.n, BN), 0, 0, linear_splits(p.m, p.n, p.k)};
+    ProductArgs g{p, 0, 0, 0, 0, linear_splits(p.m, p.n, p.k)};
     const int err = dispatch_kind(kind, [&](auto K) { return dispatch_flag(p.a_turned, [&](auto A) { return dispatch_flag(p.b_turned, [&](auto B) {
         constexpr int KIND = decltype(K)::value;
-        if constexpr (decltype(A)::value && !decltype(B)::value) return 0;
+        constexpr bool AT = decltype(A)::value, BT = decltype(B)::value;
+        if constexpr (AT && !BT) return 0;
         else {
-            const size_t depths = ceil_div(p.k, kDepth<KIND>);
-            g.depth = ceil_div(depths, g.splits);
-            g.units = g.tiles_m * g.tiles_n * g.splits;
-            return launch_args(product_kernel<KIND, decltype(A)::value, decltype(B)::value, BM, BN, 2, 2>, dim3(grid_of(g.units)), dim3(256), 0,
-                               stream, g);
+            g.depth = ceil_div(ceil_div(p.k, kDepth<KIND>), g.splits);
+            const bool fast = direct(p.a, AT, p.m, kWidth<KIND>, 256) && direct(p.b, BT, p.n, kWidth<KIND>, 256);
+            if constexpr (KIND != kF32)
+                if (fast && ceil_div(p.m, 256) * ceil_div(p.n, 256) >= 200) return launch_tiles<KIND, AT, BT, 256, 256, 2, 4, true>(g, stream);
+            return fast ? launch_tiles<KIND, AT, BT, 128, 128, 2, 2, true>(g, stream)
+                        : launch_tiles<KIND, AT, BT, 128, 128, 2, 2, false>(g, stream);
         }
     }); }); });
     if (err || g.splits == 1) return err;

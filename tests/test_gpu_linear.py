@@ -76,7 +76,8 @@ SHAPES = [(1, 1, 1, 0, 0, "bf16"), (1, 8, 8, 0, 0, "f16"), (3, 7, 5, 0, 0, "f32"
           (127, 129, 131, 0, 0, "bf16"), (128, 128, 128, 0, 0, "bf16"), (129, 512, 256, 8, 0, "f16"), (130, 72, 264, 8, 8, "bf16"),
           (200, 96, 1000, 5, 3, "f32"), (256, 320, 256, 0, 0, "bf16"), (257, 4097, 65, 0, 0, "bf16"), (300, 520, 776, 0, 0, "f16"),
           (2, 5000, 16, 0, 0, "f32"), (33, 4096, 1000, 0, 0, "f32"), (31, 2048, 2064, 0, 0, "bf16"), (512, 1024, 768, 0, 0, "bf16"),
-          (1000, 264, 1032, 0, 0, "bf16"), (2049, 136, 520, 3, 0, "bf16"), (700, 2049, 2050, 0, 0, "f16"), (1024, 512, 2048, 0, 0, "bf16")]
+          (1000, 264, 1032, 0, 0, "bf16"), (2049, 136, 520, 3, 0, "bf16"), (700, 2049, 2050, 0, 0, "f16"), (1024, 512, 2048, 0, 0, "bf16"),
+          (3608, 136, 3592, 0, 0, "bf16"), (3600, 3592, 72, 0, 0, "f16"), (200, 3592, 3608, 8, 0, "bf16"), (64, 3840, 3840, 0, 0, "f16")]
 
 
 def whole_numbers(r, rows, cols, most):
