@@ -73,16 +73,24 @@ template <int KIND, bool TURNED, int ROWS, int LANES> struct Stage {
         const size_t at = TURNED ? (k0 + d) * m.stride + row0 + r : (row0 + r) * m.stride + k0 + d;
         return load_chunk<KIND>((const char*)m.data + at * kWidth<KIND>, right <= 0 || deep <= 0 ? 0 : TURNED ? right : deep);
     }
-    // Bytes from the tile's first element to chunk i.  Rows behind the last of `rows` from the tile's first on repeat it: what they
-    // give is not stored.
+    // The fast ways: every chunk is loaded whole, from 32-bit offsets to one address.  `rows` are there from the tile's first on; rows
+    // behind them repeat the last: what they give is not stored.  Turned, the last chunk of the rows begins early, so that it ends
+    // with them, and is moved up in registers; where that is in front of the tile, the address is that much lower.
+    static __device__ __forceinline__ int lower(size_t rows) { return TURNED ? max(kChunk<KIND> - (int)min(rows, (size_t)ROWS), 0) : 0; }
+    // What chunk i is moved up by.
+    static __device__ __forceinline__ int early(size_t rows, int i)
+    {
+        return max(row(i) - ((int)min(rows, (size_t)ROWS) - kChunk<KIND>), 0);
+    }
     static __device__ __forceinline__ uint32_t offset(size_t stride, size_t rows, int i)
     {
-        const uint32_t r = (uint32_t)min((size_t)row(i), rows - (TURNED ? kChunk<KIND> : 1)), d = depth(i), step = (uint32_t)stride;
+        const int r = TURNED ? row(i) - early(rows, i) + lower(rows) : (int)min((size_t)row(i), rows - 1);
+        const uint32_t step = (uint32_t)stride, d = depth(i);
         return (TURNED ? d * step + r : r * step + d) * (uint32_t)kWidth<KIND>;
     }
-    static __device__ __forceinline__ const char* first(const ConstRows& m, size_t row0, size_t k0)
+    static __device__ __forceinline__ const char* first(const ConstRows& m, size_t row0, size_t k0, size_t rows)
     {
-        return (const char*)m.data + (TURNED ? k0 * m.stride + row0 : row0 * m.stride + k0) * kWidth<KIND>;
+        return (const char*)m.data + (TURNED ? k0 * m.stride + row0 - lower(rows) : row0 * m.stride + k0) * kWidth<KIND>;
     }
     static __device__ __forceinline__ size_t step(const ConstRows& m) { return TURNED ? m.stride * kRowBytes : kRowBytes; }
 };
@@ -92,6 +100,26 @@ template <int KIND, bool TURNED, int ROWS, int LANES> struct Stage {
 template <int TO> __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t to)
 {
     asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(base), "v"(offset), "s"(to), "i"(TO) : "memory", "scc");
+}
+// The chunk's elements from `by` on come to its front.
+template <int KIND> __device__ __forceinline__ void move_up(u32x4& q, int by)
+{
+    #pragma unroll
+    for (int step = 2; step; step /= 2) {
+        const bool go = by & (KIND == kF32 ? step : 2 * step);
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t from = q[i + step < 4 ? i + step : 3];
+            q[i] = go ? from : q[i];
+        }
+    }
+    if constexpr (KIND != kF32) {
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t next = q[i < 3 ? i + 1 : 3], own = q[i];
+            q[i] = by & 1 ? own >> 16 | next << 16 : own;
+        }
+    }
 }
 // f(std::integral_constant<int, i>) for every i below N.
 template <int... I, typename F> __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f)
@@ -187,9 +215,13 @@ constexpr size_t kBand = 8;
 constexpr int kStagePitch = 64 + 4;            // floats of a row of a wavefront's results in the LDS
 
 // One workgroup for a tile of BM x BN results, WM x WN wavefronts with 64 columns each.
-// DIRECT: whole chunks begin on 16 bytes, so tiles of k go straight into the LDS, two of them in flight; while a wavefront multiplies
-// one half of a tile it reads the next half.  Otherwise, and for a last part of a tile, through registers.
-template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN, bool DIRECT>
+// WAY kDirect: whole chunks begin on 16 bytes, so tiles of k go straight into the LDS, two of them in flight; while a wavefront
+// multiplies one half of a tile it reads the next half.
+// kThrough: chunks begin on any element; a tile waits in registers while the one before is multiplied.
+// kGuarded: rows shorter than a chunk, tiles of more than 2^31 bytes; every chunk is looked at.  So is the last part of a tile of k
+// in the other two.
+enum { kDirect, kThrough, kGuarded };
+template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN, int WAY>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
 {
     constexpr int kLanes = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, kOut = TM < 4 ? TM : 4;
@@ -242,7 +274,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
             for (int c = 0; c < StageB::kCount; ++c)
                 *(__attribute__((address_space(3))) u32x4*)(to + BM * kRowBytes + c * kLanes * 16) = rb[c];
         };
-        if constexpr (DIRECT) {
+        if constexpr (WAY != kGuarded) {
             if (const size_t rest = last > first ? (last - first) % kDepth<KIND> : 0) {      // in front: a sum has no order
                 u32x4 ra[StageA::kCount], rb[StageB::kCount];
                 fetch(ra, rb, last - rest);
@@ -264,8 +296,49 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
                 for (int c = 0; c < StageA::kCount; ++c) oa[c] = StageA::offset(p.a.stride, p.m - m0, c);
                 #pragma unroll
                 for (int c = 0; c < StageB::kCount; ++c) ob[c] = StageB::offset(p.b.stride, p.n - n0, c);
-                const char *from_a = StageA::first(p.a, m0, first), *from_b = StageB::first(p.b, n0, first);
+                const char *from_a = StageA::first(p.a, m0, first, p.m - m0), *from_b = StageB::first(p.b, n0, first, p.n - n0);
                 const size_t step_a = StageA::step(p.a), step_b = StageB::step(p.b);
+                if constexpr (WAY == kThrough) {
+                    u32x4 ra[StageA::kCount], rb[StageB::kCount];
+                    auto load = [&] {
+                        #pragma unroll
+                        for (int c = 0; c < StageA::kCount; ++c) ra[c] = *(const u32x4_a2*)(from_a + oa[c]);
+                        #pragma unroll
+                        for (int c = 0; c < StageB::kCount; ++c) rb[c] = *(const u32x4_a2*)(from_b + ob[c]);
+                        from_a += step_a;
+                        from_b += step_b;
+                    };
+                    auto settled = [&] {                        // the tile at the rows' end
+                        if (AT && p.m - m0 < BM) {
+                            #pragma unroll
+                            for (int c = 0; c < StageA::kCount; ++c) move_up<KIND>(ra[c], StageA::early(p.m - m0, c));
+                        }
+                        if (BT && p.n - n0 < BN) {
+                            #pragma unroll
+                            for (int c = 0; c < StageB::kCount; ++c) move_up<KIND>(rb[c], StageB::early(p.n - n0, c));
+                        }
+                    };
+                    load();
+                    settled();
+                    put(ra, rb, 0);
+                    if (whole > 1) load();
+                    int at = 0;
+                    for (size_t k = whole; k; --k, at ^= 1) {
+                        barrier_lds();
+                        PieceA pa;
+                        PieceB pb;
+                        read(pa, pb, at, 0);
+                        if (k > 1) {
+                            settled();
+                            put(ra, rb, at ^ 1);
+                        }
+                        if (k > 2) load();
+                        add(pa, pb);
+                        read(pa, pb, at, 1);
+                        add(pa, pb);
+                    }
+                    __syncthreads();
+                } else {
                 const uint32_t place = (uint32_t)(uintptr_t)tile + wave * 1024;
                 auto load = [&](int at) {
                     const uint32_t to = place + at * kTileBytes;
@@ -296,6 +369,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
                     __builtin_amdgcn_sched_barrier(0);
                     add(a1, b1);
                     __builtin_amdgcn_sched_barrier(0);
+                }
                 }
             }
         } else {
@@ -347,19 +421,22 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
     }
 }
 
-// Whether every chunk of an operand lies on 16 bytes and a tile's chunks within 32 bits of its first.
-bool direct(const ConstRows& m, bool turned, size_t rows, size_t width, size_t tile)
+// Whether an operand's rows hold whole chunks and a tile's chunks lie within 31 bits of its first; and whether on 16 bytes.
+bool in_chunks(const ConstRows& m, bool turned, size_t rows, size_t width)
 {
-    return (uintptr_t)m.data % 16 == 0 && m.stride * width % 16 == 0 && (!turned || rows * width % 16 == 0)
-        && m.stride < (size_t{1} << 31) / width / std::max<size_t>(tile, kRowBytes);
+    return (!turned || rows * width >= 16) && m.stride < (size_t{1} << 31) / width / 256;
+}
+bool direct(const ConstRows& m, bool turned, size_t rows, size_t width)
+{
+    return (uintptr_t)m.data % 16 == 0 && m.stride * width % 16 == 0 && (!turned || rows * width % 16 == 0);
 }
 
-template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN, bool DIRECT> int launch_tiles(ProductArgs g, void* stream)
+template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN, int WAY> int launch_tiles(ProductArgs g, void* stream)
 {
     g.tiles_m = ceil_div(g.p.m, BM);
     g.tiles_n = ceil_div(g.p.n, BN);
     g.units = g.tiles_m * g.tiles_n * g.splits;
-    return launch_args(product_kernel<KIND, AT, BT, BM, BN, WM, WN, DIRECT>, dim3(grid_of(g.units)), dim3(64 * WM * WN), 0, stream, g);
+    return launch_args(product_kernel<KIND, AT, BT, BM, BN, WM, WN, WAY>, dim3(grid_of(g.units)), dim3(64 * WM * WN), 0, stream, g);
 }
 
 }  // namespace
@@ -372,12 +449,15 @@ int launch_product(const Product& p, int kind, void* stream)
         constexpr bool AT = decltype(A)::value, BT = decltype(B)::value;
         if constexpr (AT && !BT) return 0;
         else {
+            constexpr size_t W = kWidth<KIND>;
             g.depth = ceil_div(ceil_div(p.k, kDepth<KIND>), g.splits);
-            const bool fast = direct(p.a, AT, p.m, kWidth<KIND>, 256) && direct(p.b, BT, p.n, kWidth<KIND>, 256);
-            if constexpr (KIND != kF32)
-                if (fast && ceil_div(p.m, 256) * ceil_div(p.n, 256) >= 200) return launch_tiles<KIND, AT, BT, 256, 256, 2, 4, true>(g, stream);
-            return fast ? launch_tiles<KIND, AT, BT, 128, 128, 2, 2, true>(g, stream)
-                        : launch_tiles<KIND, AT, BT, 128, 128, 2, 2, false>(g, stream);
+            if (!in_chunks(p.a, AT, p.m, W) || !in_chunks(p.b, BT, p.n, W)) return launch_tiles<KIND, AT, BT, 128, 128, 2, 2, kGuarded>(g, stream);
+            return dispatch_flag(direct(p.a, AT, p.m, W) && direct(p.b, BT, p.n, W), [&](auto D) {
+                constexpr int WAY = decltype(D)::value ? kDirect : kThrough;
+                if constexpr (KIND != kF32)
+                    if (ceil_div(p.m, 256) * ceil_div(p.n, 256) >= 200) return launch_tiles<KIND, AT, BT, 256, 256, 2, 4, WAY>(g, stream);
+                return launch_tiles<KIND, AT, BT, 128, 128, 2, 2, WAY>(g, stream);
+            });
         }
     }); }); });
     if (err || g.splits == 1) return err;
