@@ -145,7 +145,7 @@ __device__ __forceinline__ void load_codes(const char* p, int valid, float scale
     restored(q.y, scale, v + 4);
 }
 
-// z = v + bias and everything after it, for vector c of a row of which `valid` elements exist.
+// z = v + bias and everything after it, for vector c of a row of which `valid` elements exist; all lanes of a block come here.
 template <int KIND>
 __device__ __forceinline__ void finish(const Epilogue& e, size_t row, unsigned c, unsigned cols, int valid, float (&v)[kVec])
 {
@@ -159,7 +159,7 @@ __device__ __forceinline__ void finish(const Epilogue& e, size_t row, unsigned c
     if (e.codes.data) {
         uint32_t top = 0;
         #pragma unroll
-        for (int i = 0; i < kVec; ++i) top = max(top, magnitude(v[i]));
+        for (int i = 0; i < kVec; ++i) top = max(top, i < valid ? magnitude(v[i]) : 0u);
         const Coding code = coding_of(max_of_8(top));
         u32x2 q{};
         #pragma unroll

@@ -1,4 +1,4 @@
-// Activations with their 8-bit checkpoints, forward and backward, and the join of a product's parts.
+// Activations with their 8-bit checkpoints, forward and backward.
 #include "rows.h"
 
 #include <algorithm>
@@ -16,7 +16,7 @@ struct ActivationArgs {
     ActivationPass a;
     size_t groups;                             // lanes of a row
 };
-template <int KIND, bool PARTS>
+template <int KIND>
 __global__ __launch_bounds__(kActLanes) void activation_kernel(ActivationArgs p)
 {
     const ActivationPass& a = p.a;
@@ -29,19 +29,7 @@ __global__ __launch_bounds__(kActLanes) void activation_kernel(ActivationArgs p)
         const size_t row = row0 + up;
         const int valid = valid_at(c, a.cols);
         float v[kVec];
-        if constexpr (PARTS) {
-            const size_t size = a.rows * a.cols;
-            const char* const from = (const char*)(a.parts + row * a.cols + (size_t)c * kVec);
-            unpack<kF32>(load_vec<kF32>(from, valid), v);
-            for (int s = 1; s < a.splits; ++s) {
-                float t[kVec];
-                unpack<kF32>(load_vec<kF32>(from + s * size * 4, valid), t);
-                #pragma unroll
-                for (int i = 0; i < kVec; ++i) v[i] += t[i];
-            }
-        } else {
-            unpack<KIND>(load_vec<KIND>(row_at<KIND>(a.x, row) + (size_t)c * (kVec * kWidth<KIND>), valid), v);
-        }
+        unpack<KIND>(load_vec<KIND>(row_at<KIND>(a.x, row) + (size_t)c * (kVec * kWidth<KIND>), valid), v);
         finish<KIND>(a.e, row, c, a.cols, valid, v);
     }
 }
@@ -142,9 +130,9 @@ int launch_activation(const ActivationPass& a, int kind, void* stream)
 {
     const ActivationArgs p{a, row_lanes(a.cols)};
     const dim3 grid(grid_of((a.rows * p.groups + kActLanes - 1) / kActLanes));
-    return dispatch_kind(kind, [&](auto K) { return dispatch_flag(!a.x.data, [&](auto P) {
-        return launch_args(activation_kernel<decltype(K)::value, decltype(P)::value>, grid, dim3(kActLanes), 0, stream, p);
-    }); });
+    return dispatch_kind(kind, [&](auto K) {
+        return launch_args(activation_kernel<decltype(K)::value>, grid, dim3(kActLanes), 0, stream, p);
+    });
 }
 
 int launch_checkpoint_read(const CheckpointRead& a, int kind, void* stream)

@@ -35,19 +35,17 @@ template <int KIND> __device__ __forceinline__ int twist(int k)
 // One chunk of an operand, elements from `valid` on are 0.
 template <int KIND> __device__ __forceinline__ u32x4 load_chunk(const char* p, ptrdiff_t valid)
 {
-    u32x4 q{};
-    if (valid >= kChunk<KIND>) {
-        if constexpr (KIND == kF32) q = *(const u32x4_a4*)p;
-        else q = *(const u32x4_a2*)p;
-    } else {
-        #pragma unroll
-        for (int i = 0; i < kChunk<KIND>; ++i)
-            if (i < valid) {
-                if constexpr (KIND == kF32) q[i] = ((const uint32_t*)p)[i];
-                else q[i / 2] |= (uint32_t)((const uint16_t*)p)[i] << (i % 2 * 16);
-            }
+    if constexpr (KIND != kF32) return load_vec<KIND>(p, (int)min(valid, (ptrdiff_t)kVec)).q[0];
+    else {
+        u32x4 q{};
+        if (valid >= 4) q = *(const u32x4_a4*)p;
+        else if (valid > 0) {
+            q.x = *(const uint32_t*)p;
+            if (valid > 1) q.y = ((const uint32_t*)p)[1];
+            if (valid > 2) q.z = ((const uint32_t*)p)[2];
+        }
+        return q;
     }
-    return q;
 }
 
 // How the lanes of a workgroup bring a tile of ROWS rows into the LDS: chunk i * LANES + lane in the order of the places there.
@@ -197,21 +195,45 @@ template <int KIND> __device__ __forceinline__ void multiply(f32x4& acc, const P
 
 struct ProductArgs {
     Product p;
-    size_t tiles_m, tiles_n, units;            // units: tiles times splits
-    size_t depth;                              // tiles of k in a split
-    int splits;
+    unsigned bm, bn, tiles_m, tiles_n;
+    unsigned units, whole, shared, splits;     // units: whole tiles and parts of the shared ones
+    size_t depth;                              // k of a part
+    size_t a_rows, b_rows;                     // m and n, or so many elements as rows of a turned copy have
 };
 
 // The unit that a workgroup takes: neighbours on one of the 8 L2 caches (workgroups go round them) share rows of the operands.
-__device__ __forceinline__ size_t unit_of(size_t i, size_t units)
+__device__ __forceinline__ unsigned unit_of(unsigned i, unsigned units)
 {
-    const size_t each = units / 8, rest = units % 8, cache = i % 8;
+    const unsigned each = units / 8, rest = units % 8, cache = i % 8;
     return cache * each + min(cache, rest) + i / 8;
 }
 
 // Tiles of rows that are taken together, column by column: what runs at one time under one of the 8 L2 caches is then 8 x 4 tiles.
 // us, 4 / 8 / 16 rows of tiles / all: 4096 x 8192 x 32768 bf16 1673 / 1678 / 1904 / 1909, 8192 x 8192 x 8192 846 / 842 / 859 / 1167.
-constexpr size_t kBand = 8;
+constexpr unsigned kBand = 8;
+// The first row and column of tile t.
+struct Origin {
+    size_t m, n;
+};
+__device__ __forceinline__ Origin origin_of(const ProductArgs& g, unsigned t)
+{
+    const unsigned of_band = kBand * g.tiles_n, band = t / of_band, in_band = t % of_band, high = min(kBand, g.tiles_m - band * kBand);
+    return {(size_t)(band * kBand + in_band % high) * g.bm, (size_t)(in_band / high) * g.bn};
+}
+// What workgroup i computes: the tile, its part of k, and where a part goes.
+struct Unit {
+    unsigned tile;
+    size_t first, last;                        // of k
+    float* parts;                              // NULL: the whole tile
+};
+__device__ __forceinline__ Unit unit_at(const ProductArgs& g, unsigned i)
+{
+    if (i < g.whole) return {unit_of(i, g.whole), 0, g.p.k, nullptr};
+    const unsigned j = unit_of(i - g.whole, g.units - g.whole), split = j / g.shared, at = j % g.shared;
+    const size_t first = split * g.depth;
+    return {g.whole + at, first, min(g.p.k, first + g.depth), g.p.parts + ((size_t)at * g.splits + split) * (g.bm * g.bn)};
+}
+
 constexpr int kStagePitch = 64 + 4;            // floats of a row of a wavefront's results in the LDS
 
 // One workgroup for a tile of BM x BN results, WM x WN wavefronts with 64 columns each.
@@ -235,13 +257,10 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
     const int wm = wave / WN, wn = wave % WN;
     lds_char* const tile = (lds_char*)lds;
 
-    for (size_t i = blockIdx.x; i < g.units; i += gridDim.x) {
-        const size_t unit = unit_of(i, g.units), tiles = g.tiles_m * g.tiles_n;
-        const size_t split = unit / tiles, t = unit % tiles;
-        const size_t band = t / (kBand * g.tiles_n), in_band = t % (kBand * g.tiles_n), high = min(kBand, g.tiles_m - band * kBand);
-        const size_t m0 = (band * kBand + in_band % high) * BM, n0 = in_band / high * BN;
-        size_t first = split * g.depth * kDepth<KIND>;
-        const size_t last = min(p.k, first + g.depth * kDepth<KIND>);
+    for (unsigned i = blockIdx.x; i < g.units; i += gridDim.x) {
+        const Unit unit = unit_at(g, i);
+        const Origin origin = origin_of(g, unit.tile);
+        const size_t m0 = origin.m, n0 = origin.n, first = unit.first, last = unit.last;
         f32x4 acc[TM][TN] = {};
         typedef Piece<KIND> PieceA[TM];
         typedef Piece<KIND> PieceB[TN];
@@ -293,10 +312,10 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
             if (whole) {
                 uint32_t oa[StageA::kCount], ob[StageB::kCount];
                 #pragma unroll
-                for (int c = 0; c < StageA::kCount; ++c) oa[c] = StageA::offset(p.a.stride, p.m - m0, c);
+                for (int c = 0; c < StageA::kCount; ++c) oa[c] = StageA::offset(p.a.stride, g.a_rows - m0, c);
                 #pragma unroll
-                for (int c = 0; c < StageB::kCount; ++c) ob[c] = StageB::offset(p.b.stride, p.n - n0, c);
-                const char *from_a = StageA::first(p.a, m0, first, p.m - m0), *from_b = StageB::first(p.b, n0, first, p.n - n0);
+                for (int c = 0; c < StageB::kCount; ++c) ob[c] = StageB::offset(p.b.stride, g.b_rows - n0, c);
+                const char *from_a = StageA::first(p.a, m0, first, g.a_rows - m0), *from_b = StageB::first(p.b, n0, first, g.b_rows - n0);
                 const size_t step_a = StageA::step(p.a), step_b = StageB::step(p.b);
                 if constexpr (WAY == kThrough) {
                     u32x4 ra[StageA::kCount], rb[StageB::kCount];
@@ -308,8 +327,8 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
                         from_a += step_a;
                         from_b += step_b;
                     };
-                    auto settled = [&] {                        // the tile at the rows' end
-                        if (AT && p.m - m0 < BM) {
+                    auto place = [&](int at) {
+                        if (AT && p.m - m0 < BM) {              // the tile at the rows' end
                             #pragma unroll
                             for (int c = 0; c < StageA::kCount; ++c) move_up<KIND>(ra[c], StageA::early(p.m - m0, c));
                         }
@@ -317,22 +336,19 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
                             #pragma unroll
                             for (int c = 0; c < StageB::kCount; ++c) move_up<KIND>(rb[c], StageB::early(p.n - n0, c));
                         }
+                        put(ra, rb, at);
                     };
                     load();
-                    settled();
-                    put(ra, rb, 0);
+                    place(0);
                     if (whole > 1) load();
                     int at = 0;
-                    for (size_t k = whole; k; --k, at ^= 1) {
+                    for (size_t left = whole; left; --left, at ^= 1) {
                         barrier_lds();
                         PieceA pa;
                         PieceB pb;
                         read(pa, pb, at, 0);
-                        if (k > 1) {
-                            settled();
-                            put(ra, rb, at ^ 1);
-                        }
-                        if (k > 2) load();
+                        if (left > 1) place(at ^ 1);
+                        if (left > 2) load();
                         add(pa, pb);
                         read(pa, pb, at, 1);
                         add(pa, pb);
@@ -396,16 +412,16 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
         // A wavefront's results pass through the LDS into rows of 64 columns, eight to a lane.
         typedef __attribute__((address_space(3))) f32x4 lds_f4;
         lds_char* const mine = tile + wave * kOut * 16 * kStagePitch * 4;
+        __syncthreads();
         #pragma unroll
         for (int part = 0; part < TM / kOut; ++part) {
-            __syncthreads();
             #pragma unroll
             for (int m = 0; m < kOut; ++m) {
                 #pragma unroll
                 for (int n = 0; n < TN; ++n)
                     *(lds_f4*)(mine + ((m * 16 + lane % 16) * kStagePitch + n * 16 + lane / 16 * 4) * 4) = acc[part * kOut + m][n];
             }
-            __syncthreads();
+            // its own LDS accesses are in order
             for (int r = lane / 8; r < kOut * 16; r += 8) {
                 const size_t row = m0 + wm * TM * 16 + part * kOut * 16 + r, col = n0 + wn * TN * 16 + lane % 8 * kVec;
                 if (row >= p.m) break;
@@ -413,7 +429,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
                 const f32x4 low = *(const lds_f4*)from, high = *(const lds_f4*)(from + 16);
                 float v[kVec] = {low.x, low.y, low.z, low.w, high.x, high.y, high.z, high.w};
                 const int valid = col < p.n ? (int)min(p.n - col, (size_t)kVec) : 0;
-                if (g.splits > 1) store_vec<kF32>((char*)(p.parts + (split * p.m + row) * p.n + col), pack<kF32>(v), valid);
+                if (unit.parts) store_vec<kF32>((char*)(unit.parts + (row - m0) * BN + (col - n0)), pack<kF32>(v), kVec);
                 else finish<KIND>(p.e, row, (unsigned)(col / kVec), (unsigned)p.n, valid, v);
             }
         }
@@ -421,47 +437,250 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
     }
 }
 
-// Whether an operand's rows hold whole chunks and a tile's chunks lie within 31 bits of its first; and whether on 16 bytes.
-bool in_chunks(const ConstRows& m, bool turned, size_t rows, size_t width)
+// Products of few rows: all that counts is that the weights are read once, as fast as memory gives them.  A workgroup takes BN
+// columns; its wavefronts take turns at the tiles of k, 128 bytes of each row of b at a time, straight into the operands of the
+// matrix instructions, and their sums are added in the LDS.
+//   b not turned   16 columns to an instruction, lane i of 16 has chunk lane / 16 of row i;
+//   b turned       a lane has a chunk of columns of kChunk k, which it turns around in registers: instruction j takes column j of
+//                  every chunk.
+constexpr int kFewWaves = 8;
+template <int KIND, bool BT, int TM, int BN>
+__global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(ProductArgs g)
 {
-    return (!turned || rows * width >= 16) && m.stride < (size_t{1} << 31) / width / 256;
-}
-bool direct(const ConstRows& m, bool turned, size_t rows, size_t width)
-{
-    return (uintptr_t)m.data % 16 == 0 && m.stride * width % 16 == 0 && (!turned || rows * width % 16 == 0);
+    constexpr int C = kChunk<KIND>, NF = BN / 16, BM = TM * 16, kPitch = BN + 4;
+    static_assert(!BT || NF == C, "");
+    __shared__ __attribute__((aligned(16))) float sums[kFewWaves][BM * kPitch];
+    const Product& p = g.p;
+    const int wave = wave_index(), lane = threadIdx.x & 63, i16 = lane % 16, g4 = lane / 16;
+    for (unsigned i = blockIdx.x; i < g.units; i += gridDim.x) {
+        const Unit unit = unit_at(g, i);
+        const size_t n0 = (size_t)unit.tile * BN;
+        const char* a_row[TM];
+        #pragma unroll
+        for (int m = 0; m < TM; ++m) a_row[m] = (const char*)p.a.data + min((size_t)(m * 16 + i16), p.m - 1) * p.a.stride * kWidth<KIND>;
+        // turned: the last chunk of a row of b begins early and is moved up
+        const size_t column = n0 + (size_t)i16 * C, start = BT ? min(column, p.n - C) : 0;
+        const int early = (int)min(column - start, (size_t)C);
+        const char* b_row[BT ? 1 : NF];
+        if constexpr (BT) b_row[0] = (const char*)p.b.data + start * kWidth<KIND>;
+        else {
+            #pragma unroll
+            for (int n = 0; n < NF; ++n) b_row[n] = (const char*)p.b.data + min(n0 + n * 16 + i16, p.n - 1) * p.b.stride * kWidth<KIND>;
+        }
+        f32x4 acc[TM][NF] = {};
+        // one half of a tile of k from k0 on, of which the first `there` are there
+        auto half = [&](size_t k0, auto all, size_t there) {
+            constexpr bool ALL = decltype(all)::value;
+            Piece<KIND> a[TM], b[NF];
+            const ptrdiff_t rest = (ptrdiff_t)there - g4 * C;
+            if constexpr (BT) {
+                u32x4 rows[C];
+                const char* const from = b_row[0] + (k0 + g4 * C) * p.b.stride * kWidth<KIND>;
+                const uint32_t step = (uint32_t)p.b.stride * (uint32_t)kWidth<KIND>;
+                #pragma unroll
+                for (int r = 0; r < C; ++r) {
+                    rows[r] = u32x4{};
+                    if (ALL || r < rest) rows[r] = *(const u32x4_a2*)(from + r * step);
+                }
+                if (early) {
+                    #pragma unroll
+                    for (int r = 0; r < C; ++r) move_up<KIND>(rows[r], early);
+                }
+                #pragma unroll
+                for (int n = 0; n < NF; ++n) {
+                    if constexpr (KIND == kF32) {
+                        #pragma unroll
+                        for (int r = 0; r < 4; ++r) b[n].q[r] = rows[r % C][n % 4];
+                    } else {
+                        #pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const uint32_t low = rows[(2 * r) % C][n / 2 % 4], high = rows[(2 * r + 1) % C][n / 2 % 4];
+                            b[n].q[r] = n % 2 ? low >> 16 | (high & 0xFFFF0000u) : (low & 0xFFFFu) | high << 16;
+                        }
+                    }
+                }
+            } else {
+                #pragma unroll
+                for (int n = 0; n < NF; ++n) {
+                    const char* const from = b_row[n] + (k0 + g4 * C) * kWidth<KIND>;
+                    if constexpr (ALL) b[n].q = *(const u32x4_a2*)from;
+                    else b[n].q = load_chunk<KIND>(from, rest);
+                }
+            }
+            #pragma unroll
+            for (int m = 0; m < TM; ++m) {
+                const char* const from = a_row[m] + (k0 + g4 * C) * kWidth<KIND>;
+                if constexpr (ALL) a[m].q = *(const u32x4_a2*)from;
+                else a[m].q = load_chunk<KIND>(from, rest);
+            }
+            #pragma unroll
+            for (int m = 0; m < TM; ++m) {
+                #pragma unroll
+                for (int n = 0; n < NF; ++n) multiply<KIND>(acc[m][n], a[m], b[n]);
+            }
+        };
+        size_t k0 = unit.first + (size_t)wave * kDepth<KIND>;
+        constexpr size_t turn = kFewWaves * kDepth<KIND>;
+        for (; k0 + kDepth<KIND> <= unit.last; k0 += turn) {
+            half(k0, std::true_type{}, 0);
+            half(k0 + kDepth<KIND> / 2, std::true_type{}, 0);
+        }
+        for (; k0 < unit.last; k0 += turn) {                    // the last tile of k, for one wavefront
+            half(k0, std::false_type{}, unit.last - k0);
+            if (k0 + kDepth<KIND> / 2 < unit.last) half(k0 + kDepth<KIND> / 2, std::false_type{}, unit.last - k0 - kDepth<KIND> / 2);
+        }
+        // a lane has row lane % 16 and the columns that belong to rows lane / 16 * 4 + r of the instructions' first operand
+        __syncthreads();
+        #pragma unroll
+        for (int m = 0; m < TM; ++m) {
+            float* const to = sums[wave] + (m * 16 + i16) * kPitch;
+            #pragma unroll
+            for (int n = 0; n < NF; ++n) {
+                #pragma unroll
+                for (int r = 0; r < 4; ++r) to[BT ? (g4 * 4 + r) * C + n : n * 16 + g4 * 4 + r] = acc[m][n][r];
+            }
+        }
+        __syncthreads();
+        for (int at = threadIdx.x; at < BM * BN / kVec; at += 64 * kFewWaves) {
+            const int row = at / (BN / kVec), c = at % (BN / kVec);
+            float v[kVec] = {};
+            for (int w = 0; w < kFewWaves; ++w) {
+                const float* const from = sums[w] + row * kPitch + c * kVec;
+                #pragma unroll
+                for (int e = 0; e < kVec; ++e) v[e] += from[e];
+            }
+            const size_t col = n0 + (size_t)c * kVec;
+            const int valid = col < p.n ? (int)min(p.n - col, (size_t)kVec) : 0;
+            if (unit.parts) store_vec<kF32>((char*)(unit.parts + row * BN + c * kVec), pack<kF32>(v), kVec);
+            else if ((size_t)row < p.m) finish<KIND>(p.e, row, (unsigned)(col / kVec), (unsigned)p.n, valid, v);
+        }
+        __syncthreads();
+    }
 }
 
-template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN, int WAY> int launch_tiles(ProductArgs g, void* stream)
+// The sums of the shared tiles' parts, in ascending order, and what happens to them.
+constexpr int kJoinLanes = 64;
+template <int KIND> __global__ __launch_bounds__(kJoinLanes) void join_kernel(ProductArgs g)
 {
-    g.tiles_m = ceil_div(g.p.m, BM);
-    g.tiles_n = ceil_div(g.p.n, BN);
-    g.units = g.tiles_m * g.tiles_n * g.splits;
-    return launch_args(product_kernel<KIND, AT, BT, BM, BN, WM, WN, WAY>, dim3(grid_of(g.units)), dim3(64 * WM * WN), 0, stream, g);
+    const Product& p = g.p;
+    const unsigned across = g.bn / kVec, size = g.bm * g.bn;
+    const size_t lanes = (size_t)g.shared * (size / kVec);
+    for (size_t i = (size_t)blockIdx.x * kJoinLanes + threadIdx.x; i < lanes; i += (size_t)gridDim.x * kJoinLanes) {
+        const unsigned at = (unsigned)(i / (size / kVec)), in = (unsigned)(i % (size / kVec)), r = in / across, c = in % across;
+        const Origin origin = origin_of(g, g.whole + at);
+        const size_t row = origin.m + r, col = origin.n + (size_t)c * kVec;
+        if (row >= p.m) continue;                               // whole blocks of lanes
+        const float* const from = p.parts + (size_t)at * g.splits * size + (size_t)in * kVec;
+        float v[kVec] = {};
+        #pragma unroll 4
+        for (unsigned s = 0; s < g.splits; ++s) {
+            const f32x4 low = *(const f32x4_a4*)(from + (size_t)s * size), high = *(const f32x4_a4*)(from + (size_t)s * size + 4);
+            #pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] += low[e];
+                v[e + 4] += high[e];
+            }
+        }
+        finish<KIND>(p.e, row, (unsigned)(col / kVec), (unsigned)p.n, col < p.n ? (int)min(p.n - col, (size_t)kVec) : 0, v);
+    }
+}
+
+template <int KIND, bool BT> int launch_few(const ProductArgs& g, void* stream)
+{
+    constexpr int wide = BT ? 16 * kChunk<KIND> : 64;
+    const dim3 grid(grid_of(g.units)), block(64 * kFewWaves);
+    auto go = [&](auto TM) {
+        if constexpr (!BT)
+            if (g.bn == 16) return launch_args(few_rows_kernel<KIND, BT, decltype(TM)::value, 16>, grid, block, 0, stream, g);
+        return launch_args(few_rows_kernel<KIND, BT, decltype(TM)::value, wide>, grid, block, 0, stream, g);
+    };
+    return g.bm == 16 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 2>{});
+}
+
+// Operands copied into rows on 16 bytes, chunk by chunk; blockIdx.y: which.  What is behind a row's end stays as it is.
+struct Copy {
+    const char* from;
+    char* to;
+    size_t rows, stride, chunks;               // bytes from row to row of the operand; chunks of a row of the copy
+    unsigned bytes;                            // of a row
+};
+struct CopyArgs {
+    Copy c[2];
+};
+constexpr int kCopyLanes = 256;
+template <int KIND> __global__ __launch_bounds__(kCopyLanes) void copy_kernel(CopyArgs g)
+{
+    const Copy& c = g.c[blockIdx.y];
+    const size_t all = c.rows * c.chunks;
+    for (size_t base = (size_t)blockIdx.x * kCopyLanes; base < all; base += (size_t)gridDim.x * kCopyLanes) {
+        const size_t row0 = base / c.chunks;                                    // the same in all lanes
+        const unsigned at = (unsigned)(base - row0 * c.chunks) + threadIdx.x, chunks = (unsigned)c.chunks, up = at / chunks;
+        const size_t row = row0 + up, i = base + threadIdx.x;
+        if (i >= all) break;
+        const unsigned place = (at - up * chunks) * 16;
+        const u32x4 q = load_chunk<KIND>(c.from + row * c.stride + place, (ptrdiff_t)((c.bytes - place) / kWidth<KIND>));
+        *(u32x4*)(c.to + i * 16) = q;
+    }
+}
+
+template <int KIND, bool AT, bool BT, int TILE, int WM, int WN, int WAY> int launch_tiles(const ProductArgs& g, void* stream)
+{
+    return launch_args(product_kernel<KIND, AT, BT, TILE, TILE, WM, WN, WAY>, dim3(grid_of(g.units)), dim3(64 * WM * WN), 0, stream, g);
 }
 
 }  // namespace
 
-int launch_product(const Product& p, int kind, void* stream)
+int launch_product(const Product& p, const ProductPlan& plan, int kind, void* stream)
 {
-    ProductArgs g{p, 0, 0, 0, 0, linear_splits(p.m, p.n, p.k)};
+    const size_t width = kind == kF32 ? 4 : 2;
+    ProductArgs g{p, (unsigned)plan.bm, (unsigned)plan.bn, (unsigned)ceil_div(p.m, plan.bm), (unsigned)ceil_div(p.n, plan.bn),
+                  (unsigned)(plan.whole + plan.shared * plan.splits), (unsigned)plan.whole, (unsigned)plan.shared, (unsigned)plan.splits,
+                  plan.depth * (kRowBytes / width), p.m, p.n};
+    if (plan.a_copy + plan.b_copy) {
+        char* to = (char*)(((uintptr_t)p.parts + parts_bytes(plan) + 15) / 16 * 16);
+        CopyArgs c{};
+        size_t most = 0;
+        int n = 0;
+        auto take = [&](ConstRows& m, bool turned, size_t& rows, size_t bytes) {
+            if (!bytes) return;
+            const size_t high = turned ? p.k : rows, wide = turned ? rows : p.k, stride = copy_stride(wide, width);
+            c.c[n++] = {(const char*)m.data, to, high, m.stride * width, stride * width / 16, (unsigned)(wide * width)};
+            most = std::max(most, bytes / 16);
+            m = {to, stride};
+            if (turned) rows = stride;
+            to += bytes;
+        };
+        take(g.p.a, p.a_turned, g.a_rows, plan.a_copy);
+        take(g.p.b, p.b_turned, g.b_rows, plan.b_copy);
+        const int err = dispatch_kind(kind, [&](auto K) {
+            return launch_args(copy_kernel<decltype(K)::value>, dim3(grid_of((most + kCopyLanes - 1) / kCopyLanes), (unsigned)n), dim3(kCopyLanes), 0,
+                               stream, c);
+        });
+        if (err) return err;
+    }
     const int err = dispatch_kind(kind, [&](auto K) { return dispatch_flag(p.a_turned, [&](auto A) { return dispatch_flag(p.b_turned, [&](auto B) {
         constexpr int KIND = decltype(K)::value;
         constexpr bool AT = decltype(A)::value, BT = decltype(B)::value;
+        constexpr size_t W = kWidth<KIND>;
         if constexpr (AT && !BT) return 0;
         else {
-            constexpr size_t W = kWidth<KIND>;
-            g.depth = ceil_div(ceil_div(p.k, kDepth<KIND>), g.splits);
-            if (!in_chunks(p.a, AT, p.m, W) || !in_chunks(p.b, BT, p.n, W)) return launch_tiles<KIND, AT, BT, 128, 128, 2, 2, kGuarded>(g, stream);
-            return dispatch_flag(direct(p.a, AT, p.m, W) && direct(p.b, BT, p.n, W), [&](auto D) {
+            if constexpr (!AT)
+                if (plan.few) return launch_few<KIND, BT>(g, stream);
+            if (!in_chunks(p.a, AT, p.m, p.k, W) || !in_chunks(p.b, BT, p.n, p.k, W))
+                return launch_tiles<KIND, AT, BT, 128, 2, 2, kGuarded>(g, stream);
+            return dispatch_flag(on_16(g.p.a, AT, g.a_rows, W) && on_16(g.p.b, BT, g.b_rows, W), [&](auto D) {
                 constexpr int WAY = decltype(D)::value ? kDirect : kThrough;
                 if constexpr (KIND != kF32)
-                    if (ceil_div(p.m, 256) * ceil_div(p.n, 256) >= 200) return launch_tiles<KIND, AT, BT, 256, 256, 2, 4, WAY>(g, stream);
-                return launch_tiles<KIND, AT, BT, 128, 128, 2, 2, WAY>(g, stream);
+                    if (plan.bm == 256) return launch_tiles<KIND, AT, BT, 256, 2, 4, WAY>(g, stream);
+                return launch_tiles<KIND, AT, BT, 128, 2, 2, WAY>(g, stream);
             });
         }
     }); }); });
-    if (err || g.splits == 1) return err;
-    return launch_activation({p.e, {nullptr, 0}, p.parts, g.splits, p.m, (unsigned)p.n}, kind, stream);
+    if (err || plan.splits == 1) return err;
+    return dispatch_kind(kind, [&](auto K) {
+        const size_t lanes = plan.shared * plan.bm * (plan.bn / kVec);
+        return launch_args(join_kernel<decltype(K)::value>, dim3(grid_of((lanes + kJoinLanes - 1) / kJoinLanes)), dim3(kJoinLanes), 0, stream, g);
+    });
 }
 
 }  // namespace mics

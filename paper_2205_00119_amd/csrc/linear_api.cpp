@@ -29,18 +29,17 @@ int pair(const char* fn, const void* codes, const void* scales)
 }
 size_t blocks(size_t cols) { return mics::ceil_div(cols, mics::kBlockCols); }
 
+// A plan's tiles are counted in 32 bits: more have no memory to lie in.
+int countable(const char* fn, const mics::ProductPlan& p)
+{
+    return p.whole + p.shared * p.splits < (size_t{1} << 32) ? MICS_OK : fail(MICS_ERR_UNSUPPORTED, "%s: too many rows", fn);
+}
 // rows of in_features and of out_features
 int features(const char* fn, size_t rows, size_t in, size_t out)
 {
     MICS_TRY(Checked(fn, rows, in).sizes("in_features"));
     return Checked(fn, rows, out).sizes("out_features");
 }
-size_t parts_bytes(size_t m, size_t n, size_t k)
-{
-    const int s = mics::linear_splits(m, n, k);
-    return s > 1 ? (size_t)s * m * n * 4 : 0;
-}
-
 }  // namespace
 
 extern "C" {
@@ -71,7 +70,7 @@ int mics_activation(void* y, int8_t* codes, float* scales, const void* x, const 
     MICS_TRY(args.check());
     if (rows == 0) return MICS_OK;
     a.e.scales = scales; a.e.bias = bias; a.e.act = act; a.e.param = param_dtype; a.e.out_kind = dtype;
-    a.splits = 1; a.rows = rows; a.cols = (unsigned)cols;
+    a.rows = rows; a.cols = (unsigned)cols;
     const int err = mics::launch_activation(a, dtype, stream);
     return err ? hip_fail(fn, err) : MICS_OK;
 }
@@ -131,7 +130,9 @@ int mics_activation_backward(void* dx, void* dbias, const void* dy, const void* 
 size_t mics_linear_workspace_bytes(size_t rows, size_t in, size_t out)
 {
     if (!column_sizes(rows, in) || !column_sizes(rows, out)) return 0;
-    return std::max({parts_bytes(rows, out, in), parts_bytes(rows, in, out), parts_bytes(out, in, rows)});
+    using mics::most_workspace;
+    return std::max({most_workspace(rows, out, in, false, false), most_workspace(rows, in, out, false, true),
+                     most_workspace(out, in, rows, true, true)});
 }
 
 int mics_linear(void* out, void* pre, int8_t* codes, float* scales, const void* x, const void* weight, const void* bias,
@@ -145,14 +146,17 @@ int mics_linear(void* out, void* pre, int8_t* codes, float* scales, const void* 
     MICS_TRY(activation(fn, act));
     MICS_TRY(features(fn, rows, in, outs));
     MICS_TRY(pair(fn, codes, scales));
-    const size_t e = width(dtype), needed = parts_bytes(rows, outs, in);
+    const size_t e = width(dtype);
     mics::Product p{};
+    p.m = rows; p.n = outs; p.k = in;
     p.e.out = {out, strides ? strides[0] : outs};
     p.e.pre = {pre, strides ? strides[1] : outs};
     p.e.codes = {codes, strides ? strides[2] : outs};
     p.a = {x, strides ? strides[3] : in};
     p.b = {weight, strides ? strides[4] : in};
     p.e.residual = {residual, strides ? strides[5] : outs};
+    const mics::ProductPlan plan = mics::plan_of(p, e);
+    const size_t needed = mics::workspace_of(plan);
     args.matrix("out", out, p.e.out.stride, e, true);
     args.matrix("pre", pre, p.e.pre.stride, e, true, true);
     args.matrix("codes", codes, p.e.codes.stride, 1, true, true);
@@ -164,10 +168,11 @@ int mics_linear(void* out, void* pre, int8_t* codes, float* scales, const void* 
     if (needed) args.vector("workspace", work, needed, 1, true);
     MICS_TRY(workspace(fn, work, work_bytes, needed));
     MICS_TRY(args.check());
+    MICS_TRY(countable(fn, plan));
     if (rows == 0) return MICS_OK;
     p.e.scales = scales; p.e.bias = bias; p.e.act = act; p.e.param = param_dtype; p.e.out_kind = dtype;
-    p.m = rows; p.n = outs; p.k = in; p.parts = (float*)work;
-    const int err = mics::launch_product(p, dtype, stream);
+    p.parts = (float*)work;
+    const int err = mics::launch_product(p, plan, dtype, stream);
     return err ? hip_fail(fn, err) : MICS_OK;
 }
 
@@ -178,12 +183,15 @@ int mics_linear_backward_input(void* dx, const void* dz, const void* weight, con
     Checked args(fn, rows, in);
     MICS_TRY(args.dtype("dtype", dtype));
     MICS_TRY(features(fn, rows, in, outs));
-    const size_t e = width(dtype), needed = parts_bytes(rows, in, outs);
+    const size_t e = width(dtype);
     mics::Product p{};
+    p.m = rows; p.n = in; p.k = outs; p.b_turned = true;
     p.e.out = {dx, strides ? strides[0] : in};
     p.a = {dz, strides ? strides[1] : outs};
     p.b = {weight, strides ? strides[2] : in};
     p.e.residual = {dsum, strides ? strides[3] : in};
+    const mics::ProductPlan plan = mics::plan_of(p, e);
+    const size_t needed = mics::workspace_of(plan);
     args.matrix("dx", dx, p.e.out.stride, e, true);
     args.shaped("dz", dz, rows, outs, p.a.stride, e, false, false, true);
     args.shaped("weight", weight, outs, in, p.b.stride, e, false, rows == 0, true);
@@ -191,10 +199,10 @@ int mics_linear_backward_input(void* dx, const void* dz, const void* weight, con
     if (needed) args.vector("workspace", work, needed, 1, true);
     MICS_TRY(workspace(fn, work, work_bytes, needed));
     MICS_TRY(args.check());
+    MICS_TRY(countable(fn, plan));
     if (rows == 0) return MICS_OK;
-    p.e.out_kind = dtype; p.b_turned = true;
-    p.m = rows; p.n = in; p.k = outs; p.parts = (float*)work;
-    const int err = mics::launch_product(p, dtype, stream);
+    p.e.out_kind = dtype; p.parts = (float*)work;
+    const int err = mics::launch_product(p, plan, dtype, stream);
     return err ? hip_fail(fn, err) : MICS_OK;
 }
 
@@ -206,20 +214,22 @@ int mics_linear_backward_weight(void* dweight, const void* dz, const void* x, si
     MICS_TRY(args.dtype("dtype", dtype));
     MICS_TRY(args.dtype("grad_dtype", grad_dtype));
     MICS_TRY(features(fn, rows, in, outs));
-    const size_t e = width(dtype), needed = parts_bytes(outs, in, rows);
+    const size_t e = width(dtype);
     mics::Product p{};
+    p.m = outs; p.n = in; p.k = rows; p.a_turned = p.b_turned = true;
     p.e.out = {dweight, strides ? strides[0] : in};
     p.a = {dz, strides ? strides[1] : outs};
     p.b = {x, strides ? strides[2] : in};
+    const mics::ProductPlan plan = mics::plan_of(p, e);
+    const size_t needed = mics::workspace_of(plan);
     args.matrix("dweight", dweight, p.e.out.stride, width(grad_dtype), true);
     args.shaped("dz", dz, rows, outs, p.a.stride, e, false, false, true);
     args.shaped("x", x, rows, in, p.b.stride, e, false, false, true);
     if (needed) args.vector("workspace", work, needed, 1, true);
     MICS_TRY(workspace(fn, work, work_bytes, needed));
     MICS_TRY(args.check());
-    p.e.out_kind = grad_dtype; p.a_turned = p.b_turned = true;
-    p.m = outs; p.n = in; p.k = rows; p.parts = (float*)work;
-    const int err = mics::launch_product(p, dtype, stream);
+    p.e.out_kind = grad_dtype; p.parts = (float*)work;
+    const int err = mics::launch_product(p, plan, dtype, stream);
     return err ? hip_fail(fn, err) : MICS_OK;
 }
 

@@ -26,17 +26,30 @@ struct Product {
     ConstRows a, b;
     bool a_turned, b_turned;
     size_t m, n, k;
-    float* parts;                              // [split][m][n]
+    float* parts;                              // [shared tile][split][row][column] of a plan with several splits; then copies
 };
-// One launch, and one more where linear_splits() > 1.
-int launch_product(const Product& p, int kind, void* stream);
+// Whether an operand's rows hold whole chunks of 16 bytes, and a tile's chunks lie within 31 bits of its first.
+inline bool in_chunks(const ConstRows& m, bool turned, size_t rows, size_t k, size_t width)
+{
+    return (turned ? rows : k) * width >= 16 && m.stride < (size_t{1} << 31) / width / 256;
+}
+// Whether every chunk of an operand lies on 16 bytes.
+inline bool on_16(const ConstRows& m, bool turned, size_t rows, size_t width)
+{
+    return (uintptr_t)m.data % 16 == 0 && m.stride * width % 16 == 0 && (!turned || rows * width % 16 == 0);
+}
+inline ProductPlan plan_of(const Product& p, size_t width)
+{
+    return plan_product({p.m, p.n, p.k, width, p.a_turned, p.b_turned, on_16(p.a, p.a_turned, p.m, width), on_16(p.b, p.b_turned, p.n, width),
+                         in_chunks(p.a, p.a_turned, p.m, p.k, width) && in_chunks(p.b, p.b_turned, p.n, p.k, width), p.e.codes.data != nullptr});
+}
+// One launch, and one more each where the plan copies operands or has several splits.
+int launch_product(const Product& p, const ProductPlan& plan, int kind, void* stream);
 
-// z = x + bias, or the sum of `splits` parts of packed rows (x.data NULL) + bias.
+// z = x + bias
 struct ActivationPass {
     Epilogue e;
     ConstRows x;
-    const float* parts;
-    int splits;
     size_t rows;
     unsigned cols;
 };

@@ -1,25 +1,122 @@
-// How a product is cut into tiles and parts: rules on sizes alone, host code.
+// How a product is cut into tiles and parts: rules on sizes, strides and alignment, host code.
 #pragma once
 
+#include <algorithm>
 #include <cstddef>
 
 namespace mics {
 
-constexpr size_t kLinearWorkspace = size_t{64} << 20;      // the parts of a product take no more
-constexpr size_t kTile = 128;
 constexpr size_t ceil_div(size_t a, size_t b) { return a / b + (a % b ? 1 : 0); }
 
-// Parts into which the sum over k is cut.
-constexpr int linear_splits(size_t m, size_t n, size_t k)
+constexpr size_t kLinearWorkspace = size_t{64} << 20;      // the parts of a product take no more
+constexpr size_t kFewRows = 32;                            // up to here the kernel of few rows
+constexpr size_t kCUs = 256;
+
+struct ProductShape {
+    size_t m, n, k, width;                                 // width: bytes of an element
+    bool a_turned, b_turned;
+    bool a_on_16, b_on_16;                                 // every chunk of 16 bytes lies on 16 (on_16)
+    bool chunks;                                           // rows hold whole chunks, offsets fit 31 bits (in_chunks)
+    bool blocks;                                           // a workgroup has to hold whole blocks of 64 columns
+};
+
+// `whole` tiles have one workgroup each, the `shared` ones behind them `splits`, of `depth` tiles of k (128 bytes) each.
+// Operands that are copied first, so that they lie on 16 bytes, take a_copy and b_copy bytes.
+struct ProductPlan {
+    bool few;
+    size_t bm, bn, whole, shared, splits, depth;
+    size_t a_copy, b_copy;
+};
+constexpr size_t parts_bytes(const ProductPlan& p) { return p.splits > 1 ? p.shared * p.splits * p.bm * p.bn * 4 : 0; }
+// Parts, copies, and what the first copy's place on 16 bytes may take.
+constexpr size_t workspace_of(const ProductPlan& p) { return parts_bytes(p) + (p.a_copy + p.b_copy ? p.a_copy + p.b_copy + 16 : 0); }
+// Elements of a row of a copy.
+constexpr size_t copy_stride(size_t row, size_t width) { return ceil_div(row * width, 16) * 16 / width; }
+
+// What a cut into tiles of `tile` rows and columns takes in ns, with the best number of parts for the tiles of the last round.
+// slow: what a tile of k takes against operands on 16 bytes.  Measured (us): a tile of k for all workgroups that fit, 256 x 256, one on
+// a compute unit, 1.6 (4096 x 8192 x 4096 bf16 208), 128 x 128, two on one, 0.93 (8192 x 8192 x 8192 961), one on one 0.57
+// (4096 x 8192 x 1024 78); 336 tiles of 128 x 128 with k = 5120 65, in three parts each 71, 160 of 256 x 256 with k = 2560 71;
+// beginning and end of a tile 8 and 4.
+struct TileCost {
+    ProductPlan plan;
+    double ns;
+};
+inline TileCost cost_of_tiles(const ProductShape& s, size_t tile, size_t room, double slow)
 {
-    if (m == 0 || n == 0 || k == 0) return 1;
-    const size_t tiles = ceil_div(m, kTile) * ceil_div(n, kTile);
-    if (tiles >= 256) return 1;
-    size_t s = 512 / tiles;
-    const size_t most = ceil_div(k, 256);
-    if (s > most) s = most;
-    while (s > 1 && s * m > kLinearWorkspace / 4 / n) --s;
-    return s < 1 ? 1 : (int)s;
+    const size_t tiles = ceil_div(s.m, tile) * ceil_div(s.n, tile), depths = ceil_div(s.k, 128 / s.width);
+    if (s.width == 4) slow *= 8;                           // the rates of the matrix instructions
+    const bool large = tile == 256;
+    const double full = (large ? 1600 : 930) * slow, half = (large ? 1600 : 570) * slow, ends = large ? 8000 : 4000;
+    const size_t slots = large ? kCUs : 2 * kCUs;
+    auto rounds = [&](size_t units, size_t depth) {
+        const size_t rest = units % slots;
+        double last = half;
+        if (rest > kCUs) last += (full - half) * (0.3 + 0.7 * (double)(rest - kCUs) / kCUs);
+        return (units / slots) * (depth * full + ends) + (rest ? depth * last + ends : 0);
+    };
+    TileCost best{{false, tile, tile, tiles, 0, 1, depths, 0, 0}, rounds(tiles, depths)};
+    for (const size_t shared : {tiles % slots, tiles % slots + slots}) {
+        if (shared == 0 || shared > tiles) continue;
+        for (size_t splits = 2; splits <= 64 && splits <= depths; ++splits) {
+            const size_t units = shared * splits, depth = ceil_div(depths, splits);
+            if (units > 2 * slots || units * tile * tile * 4 > room) break;
+            if (ceil_div(depths, depth) < splits) continue;
+            // the parts are written and read, and a second launch
+            const double ns = rounds(tiles - shared, depths) + rounds(units, depth) + units * tile * tile * 8 / 5000.0 + 4000;
+            if (ns < best.ns) best = {{false, tile, tile, tiles - shared, shared, splits, depth, 0, 0}, ns};
+        }
+    }
+    return best;
+}
+
+inline ProductPlan plan_product(const ProductShape& s)
+{
+    const size_t depths = ceil_div(s.k, 128 / s.width);
+    if (s.m <= kFewRows && !s.a_turned && s.chunks && depths && (s.b_turned || s.b_on_16)) {
+        const size_t bm = s.m <= 16 ? 16 : 32;
+        const size_t bn = s.b_turned ? 256 / s.width : s.blocks ? 64 : 16;
+        const size_t tiles = ceil_div(s.n, bn);
+        size_t splits = 1, depth = depths;
+        if (s.b_turned && tiles < 2 * kCUs) {              // few columns: enough workgroups for the memory's latency
+            splits = std::min(2 * kCUs / tiles, ceil_div(depths, 8));
+            depth = ceil_div(depths, splits);
+            splits = ceil_div(depths, depth);
+        }
+        return {true, bm, bn, splits > 1 ? 0 : tiles, splits > 1 ? tiles : 0, splits, depth, 0, 0};
+    }
+    auto best = [&](size_t room, double slow_128, double slow_256) {
+        const TileCost small = cost_of_tiles(s, 128, room, slow_128);
+        if (s.width == 4 || !s.chunks) return small;
+        const TileCost large = cost_of_tiles(s, 256, room, slow_256);
+        return large.ns <= small.ns ? large : small;
+    };
+    const bool off = s.chunks && !(s.a_on_16 && s.b_on_16);
+    if (!off) return best(kLinearWorkspace, 1, 1).plan;
+    // Loads off 16 bytes take the L1 cache twice the time and more.  us, binary16, so / copied first: 128 x 128, 2047 x 5121 x 2561
+    // 131 / 104, its gradients 119 / 105 and 111 / 90; 256 x 256, 4095 x 3001 x 3003 bf16 113 / 104, the weight's gradient 111 / 81;
+    // 1000 x 1001 x 1003 in two parts 20 / 25.  32-bit products are bound by the matrix instructions.
+    const TileCost own = s.width == 4 ? best(kLinearWorkspace, 1.05, 1) : best(kLinearWorkspace, 1.5, s.a_turned ? 1.8 : 1.3);
+    const size_t a = s.a_on_16 ? 0 : (s.a_turned ? s.k * copy_stride(s.m, s.width) : s.m * copy_stride(s.k, s.width)) * s.width;
+    const size_t b = s.b_on_16 ? 0 : (s.b_turned ? s.k * copy_stride(s.n, s.width) : s.n * copy_stride(s.k, s.width)) * s.width;
+    if (a > kLinearWorkspace || b > kLinearWorkspace || a + b + 16 > kLinearWorkspace) return own.plan;
+    TileCost copied = best(kLinearWorkspace - a - b - 16, 1, 1);
+    copied.ns += (a + b) / 2700.0 + 4500;
+    if (copied.ns >= own.ns) return own.plan;
+    copied.plan.a_copy = a;
+    copied.plan.b_copy = b;
+    return copied.plan;
+}
+
+// Of every type and alignment.
+inline size_t most_workspace(size_t m, size_t n, size_t k, bool a_turned, bool b_turned)
+{
+    size_t most = 0;
+    for (const size_t width : {2, 4})
+        for (int flags = 0; flags < 16; ++flags)
+            most = std::max(most, workspace_of(plan_product({m, n, k, width, a_turned, b_turned, (flags & 1) != 0, (flags & 2) != 0,
+                                                             (flags & 4) != 0, (flags & 8) != 0})));
+    return most;
 }
 
 }  // namespace mics
