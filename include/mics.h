@@ -50,8 +50,9 @@
  *     coalesced ones, which issue one per 48 to 96 tensors, backward passes
  *     that sum over rows (one with few rows or none, else two, and one more
  *     with rows of more than 8192 columns), log probabilities of few long
- *     rows (two) and products of few tiles (two): these may have enqueued
- *     earlier launches when a later one fails.
+ *     rows (two) and products whose last tiles are shared or whose operands
+ *     are copied first (one more each): these may have enqueued earlier
+ *     launches when a later one fails.
  *   - Return value: MICS_OK or a negative MICS_ERR_*; mics_last_error() gives
  *     the text for the calling thread's most recent failure.
  *   - bf16 values travel as uint16_t bit patterns (upper half of a binary32).
@@ -498,10 +499,13 @@ int mics_activation_backward(void* dx, void* dbias, const void* dy, const void* 
  *   codes, scales    of out_features columns; may be NULL, both or neither
  *   bias             out_features of param_dtype, may be NULL (0)
  *   residual         may be NULL (0), may be out
- *   workspace        mics_linear_workspace_bytes(rows, in_features, out_features), at most 64 MiB and 0 for large products:
- *                    few tiles are shared by several workgroups, whose sums a second launch joins
+ *   workspace        mics_linear_workspace_bytes(rows, in_features, out_features) serves this call and the gradients of the same
+ *                    sizes, whatever their types, strides and alignment.  Fewer rows may take more than many; no product takes
+ *                    more than MICS_LINEAR_MOST_WORKSPACE.  It holds the sums of tiles that several workgroups share, which a second
+ *                    launch joins, and copies of operands off 16 bytes, which a launch in front makes
  * out may not take the place of x or weight.  1 <= in_features, out_features <= 2^24.
  */
+#define MICS_LINEAR_MOST_WORKSPACE ((size_t)64 << 20)
 size_t mics_linear_workspace_bytes(size_t rows, size_t in_features, size_t out_features);
 int mics_linear(void* out, void* pre, int8_t* codes, float* scales, const void* x, const void* weight, const void* bias,
                 const void* residual, size_t rows, size_t in_features, size_t out_features, const size_t* strides, int act,

@@ -38,6 +38,7 @@ EXPORTS = (
 )
 MICS_MAX_TOP = 64
 MICS_CHECKPOINT_BLOCK = 64
+MICS_LINEAR_MOST_WORKSPACE = 64 << 20
 MICS_ACT_NONE, MICS_ACT_RELU, MICS_ACT_GELU, MICS_ACT_GELU_TANH, MICS_ACT_SILU = range(5)
 MICS_DTYPE_BF16, MICS_DTYPE_F16, MICS_DTYPE_F32 = 0, 1, 2
 

@@ -670,7 +670,7 @@ int launch_product(const Product& p, const ProductPlan& plan, int kind, void* st
                 return launch_tiles<KIND, AT, BT, 128, 2, 2, kGuarded>(g, stream);
             return dispatch_flag(on_16(g.p.a, AT, g.a_rows, W) && on_16(g.p.b, BT, g.b_rows, W), [&](auto D) {
                 constexpr int WAY = decltype(D)::value ? kDirect : kThrough;
-                if constexpr (KIND != kF32)
+                if constexpr (KIND != kF32 && !(AT && WAY == kThrough))
                     if (plan.bm == 256) return launch_tiles<KIND, AT, BT, 256, 2, 4, WAY>(g, stream);
                 return launch_tiles<KIND, AT, BT, 128, 2, 2, WAY>(g, stream);
             });

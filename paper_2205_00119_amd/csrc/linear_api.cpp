@@ -17,7 +17,8 @@ using mics::hip_fail;
 using mics::width;
 using mics::workspace;
 
-static_assert(MICS_CHECKPOINT_BLOCK == mics::kBlockCols && MICS_ACT_SILU + 1 == mics::kActs, "");
+static_assert(MICS_CHECKPOINT_BLOCK == mics::kBlockCols && MICS_ACT_SILU + 1 == mics::kActs
+              && MICS_LINEAR_MOST_WORKSPACE == mics::kLinearWorkspace, "");
 
 int activation(const char* fn, int act)
 {
@@ -104,7 +105,8 @@ int mics_activation_backward(void* dx, void* dbias, const void* dy, const void* 
     MICS_TRY(activation(fn, act));
     MICS_TRY(args.sizes("cols"));
     MICS_TRY(pair(fn, codes, scales));
-    if (rows && !z == !codes) return fail(MICS_ERR_INVALID_ARG, "%s: z %s codes are NULL", fn, z ? "nor" : "and");
+    if (rows && !z && !codes) return fail(MICS_ERR_INVALID_ARG, "%s: z and codes are NULL", fn);
+    if (z && codes) return fail(MICS_ERR_INVALID_ARG, "%s: z or codes has to be NULL", fn);
     if (rows && !dx && !dbias) return fail(MICS_ERR_INVALID_ARG, "%s: dx and dbias are NULL", fn);
     const size_t e = width(dtype), needed = dbias ? mics_column_workspace_bytes(rows, cols) : 0;
     mics::ActivationBackward a{};

@@ -73,6 +73,7 @@ inline TileCost cost_of_tiles(const ProductShape& s, size_t tile, size_t room, d
 inline ProductPlan plan_product(const ProductShape& s)
 {
     const size_t depths = ceil_div(s.k, 128 / s.width);
+    if (s.m == 0) return {false, 128, 128, 0, 0, 1, depths, 0, 0};
     if (s.m <= kFewRows && !s.a_turned && s.chunks && depths && (s.b_turned || s.b_on_16)) {
         const size_t bm = s.m <= 16 ? 16 : 32;
         const size_t bn = s.b_turned ? 256 / s.width : s.blocks ? 64 : 16;
@@ -85,18 +86,19 @@ inline ProductPlan plan_product(const ProductShape& s)
         }
         return {true, bm, bn, splits > 1 ? 0 : tiles, splits > 1 ? tiles : 0, splits, depth, 0, 0};
     }
-    auto best = [&](size_t room, double slow_128, double slow_256) {
+    auto best = [&](size_t room, double slow_128, double slow_256) {           // 0: no tiles of 256 x 256
         const TileCost small = cost_of_tiles(s, 128, room, slow_128);
-        if (s.width == 4 || !s.chunks) return small;
+        if (s.width == 4 || !s.chunks || slow_256 == 0) return small;
         const TileCost large = cost_of_tiles(s, 256, room, slow_256);
         return large.ns <= small.ns ? large : small;
     };
     const bool off = s.chunks && !(s.a_on_16 && s.b_on_16);
     if (!off) return best(kLinearWorkspace, 1, 1).plan;
     // Loads off 16 bytes take the L1 cache twice the time and more.  us, binary16, so / copied first: 128 x 128, 2047 x 5121 x 2561
-    // 131 / 104, its gradients 119 / 105 and 111 / 90; 256 x 256, 4095 x 3001 x 3003 bf16 113 / 104, the weight's gradient 111 / 81;
+    // 131 / 104, its gradients 119 / 105 and 111 / 90; 256 x 256, 4095 x 3001 x 3003 bf16 113 / 104, the weight's gradient above
+    // 111 / 81, so 1.8 times as long, which 128 x 128 never is;
     // 1000 x 1001 x 1003 in two parts 20 / 25.  32-bit products are bound by the matrix instructions.
-    const TileCost own = s.width == 4 ? best(kLinearWorkspace, 1.05, 1) : best(kLinearWorkspace, 1.5, s.a_turned ? 1.8 : 1.3);
+    const TileCost own = s.width == 4 ? best(kLinearWorkspace, 1.05, 0) : best(kLinearWorkspace, 1.5, s.a_turned ? 0 : 1.3);
     const size_t a = s.a_on_16 ? 0 : (s.a_turned ? s.k * copy_stride(s.m, s.width) : s.m * copy_stride(s.k, s.width)) * s.width;
     const size_t b = s.b_on_16 ? 0 : (s.b_turned ? s.k * copy_stride(s.n, s.width) : s.n * copy_stride(s.k, s.width)) * s.width;
     if (a > kLinearWorkspace || b > kLinearWorkspace || a + b + 16 > kLinearWorkspace) return own.plan;
