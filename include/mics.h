@@ -439,7 +439,7 @@ int mics_token_logprobs_backward(void* dlogits, const void* logits, const int64_
  *     GELU       z P(z), P the distribution function of the standard normal
  *     GELU_TANH  z / (1 + exp(-2 sqrt(2/pi) (z + 0.044715 z^3)))
  *     SILU       z / (1 + exp(-z))
- * NaN stays NaN (RELU too); z = -inf gives NaN as 0 * inf does, but 0 for RELU.
+ * NaN stays NaN, in slopes too; at infinities are the limits.
  */
 #define MICS_ACT_NONE      0
 #define MICS_ACT_RELU      1

@@ -14,12 +14,12 @@ enum { kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4 
 // a constant term, fitted to erfcx(|z|/sqrt 2)/2 by iterated reweighted least squares, relative error 3e-8 up to |z| = 2 and
 // 1e-6 at 13; evaluated in binary32 it is within 4.1e-7 up to 4 and 1.3e-6 up to 13.
 struct Normal {
-    float below, bell;                         // the function at -|z|; exp(-z^2/2)
+    float below, bell, near;                   // the function at -|z|; exp(-z^2/2); |z|, at most 16, where both others are 0
 };
 __device__ __forceinline__ Normal normal_at(float z)
 {
-    const float a = __builtin_fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.23f, a, 1.f));
-    const float near = __builtin_amdgcn_fmed3f(a, 0.f, 16.f);              // the bell is 0 from there on; NaN stays in t
+    const float a = __builtin_fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.23f, a, 1.f));      // keeps NaN, which `near` loses
+    const float near = fminf(a, 16.f);
     const float bell = __builtin_amdgcn_exp2f(near * (near * -0.72134752f));   // log2 e / 2
     float s = __builtin_fmaf(-0.07516629248857498f, t, 0.27394965291023254f);
     s = __builtin_fmaf(s, t, -0.2431972622871399f);
@@ -28,7 +28,7 @@ __device__ __forceinline__ Normal normal_at(float z)
     s = __builtin_fmaf(s, t, 0.10681562125682831f);
     s = __builtin_fmaf(s, t, 0.08907731622457504f);
     s = __builtin_fmaf(s, t, 0.09190764278173447f);
-    return {bell * (s * t), bell};
+    return {bell * (s * t), bell, near};
 }
 // 1 / (1 + exp(-2 sqrt(2/pi) (z + 0.044715 z^3)))
 __device__ __forceinline__ float tanh_share(float z)
@@ -37,15 +37,17 @@ __device__ __forceinline__ float tanh_share(float z)
 }
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f)); }
 
+// Factors that meet a 0 are kept finite: -inf gives 0.
 template <int ACT> __device__ __forceinline__ float act_of(float z)
 {
+    const float high = fmaxf(z, -3.4028234664e38f);
     if constexpr (ACT == kActRelu) return z <= 0.f ? 0.f : z;
     else if constexpr (ACT == kActGelu) {
-        const float q = normal_at(z).below;
-        return z * (z < 0.f ? q : 1.f - q);
+        const Normal n = normal_at(z);
+        return __builtin_fmaf(-n.near, n.below, fmaxf(z, 0.f));
     }
-    else if constexpr (ACT == kActGeluTanh) return z * tanh_share(z);
-    else if constexpr (ACT == kActSilu) return z * logistic(z);
+    else if constexpr (ACT == kActGeluTanh) return high * tanh_share(z);
+    else if constexpr (ACT == kActSilu) return high * logistic(z);
     else return z;
 }
 // Where the second factor of a product is 0 from some |z| on, the first stops growing there: no 0 * inf.
@@ -78,28 +80,38 @@ template <typename F> __device__ __forceinline__ void with_act(int act, F&& f)
 }
 
 // The scale of a block and what its elements are multiplied by.  `top`: the largest magnitude's bits, so that infinities and
-// NaN are larger than all numbers.
+// NaN are larger than all numbers; such a block's codes are masked away.  Both quotients are correctly rounded: a product with the
+// divisor's reciprocal, then its remainder, which is exact, times the reciprocal; for 127 / t the reciprocal is refined first, and
+// where it would be subnormal the division is left to the compiler.
 struct Coding {
     float scale, by;
+    uint32_t keep;
 };
 __device__ __forceinline__ Coding coding_of(uint32_t top)
 {
-    if (top > 0x7F7FFFFFu) return {__builtin_nanf(""), 0.f};
+    if (top > 0x7F7FFFFFu) return {__builtin_nanf(""), 0.f, 0u};
     const float t = fmaxf(__builtin_bit_cast(float, top), 0x1p-100f);
-    return {t / 127.f, 127.f / t};
+    constexpr float r127 = 1.f / 127.f;
+    const float q = t * r127, scale = __builtin_fmaf(__builtin_fmaf(-127.f, q, t), r127, q);
+    if (t > 0x1p100f) return {scale, 127.f / t, ~0u};
+    const float y = __builtin_amdgcn_rcpf(t), r = __builtin_fmaf(__builtin_fmaf(-t, y, 1.f), y, y), p = 127.f * r;
+    return {scale, __builtin_fmaf(__builtin_fmaf(-t, p, 127.f), r, p), ~0u};
 }
-__device__ __forceinline__ uint32_t magnitude(float z) { return __builtin_bit_cast(uint32_t, z) & 0x7FFFFFFFu; }
-// rint(z * by) in the low 8 bits: of a number of at most 127 with 1.5 * 2^23 added the last bit counts ones.  A block that stands for
-// NaN multiplies by 0 what may be infinite, so its codes are made 0.
-__device__ __forceinline__ uint32_t code_of(float z, const Coding& c)
+// rint(z * by) in the low 8 bits: of a number of at most 127 with 1.5 * 2^23 added the last bit counts ones.
+__device__ __forceinline__ uint32_t code_of(float z, float by) { return __builtin_bit_cast(uint32_t, z * by + 12582912.f); }
+__device__ __forceinline__ uint32_t codes_of(const float* z, const Coding& c)
 {
-    return c.by != 0.f ? __builtin_bit_cast(uint32_t, z * c.by + 12582912.f) & 0xFFu : 0u;
+    const uint32_t low = __builtin_amdgcn_perm(code_of(z[1], c.by), code_of(z[0], c.by), 0x0C0C0400u);
+    const uint32_t high = __builtin_amdgcn_perm(code_of(z[3], c.by), code_of(z[2], c.by), 0x0C0C0400u);
+    return __builtin_amdgcn_perm(high, low, 0x05040100u) & c.keep;
 }
-// Four codes; what they stand for.
+// What four codes stand for: of code + 128, times the scale, 128 scales are taken away, which rounds once as code * scale does.
 __device__ __forceinline__ void restored(uint32_t codes, float scale, float* v)
 {
+    const uint32_t u = codes ^ 0x80808080u;
+    const float off = -128.f * scale;
     #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (float)((int32_t)(codes << (24 - 8 * i)) >> 24) * scale;
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf((float)(uint8_t)(u >> (8 * i)), scale, off);
 }
 
 typedef u32x2 u32x2_a1 __attribute__((aligned(1)));
@@ -132,7 +144,7 @@ __device__ __forceinline__ void store_any(char* row, int kind, unsigned c, int v
     else if (kind == kF16) store_vec<kF16>(row + (size_t)c * 16, pack<kF16>(v), valid);
     else store_vec<kF32>(row + (size_t)c * 32, pack<kF32>(v), valid);
 }
-__device__ __forceinline__ void load_codes(const char* p, int valid, float scale, float (&v)[kVec])
+__device__ __forceinline__ u32x2 load_codes(const char* p, int valid)
 {
     u32x2 q{};
     if (valid >= kVec) q = *(const u32x2_a1*)p;
@@ -141,8 +153,7 @@ __device__ __forceinline__ void load_codes(const char* p, int valid, float scale
             const uint32_t b = (uint32_t)(uint8_t)p[i] << (i % 4 * 8);
             if (i < 4) q.x |= b; else q.y |= b;
         }
-    restored(q.x, scale, v);
-    restored(q.y, scale, v + 4);
+    return q;
 }
 
 // z = v + bias and everything after it, for vector c of a row of which `valid` elements exist; all lanes of a block come here.
@@ -157,13 +168,16 @@ __device__ __forceinline__ void finish(const Epilogue& e, size_t row, unsigned c
     }
     if (e.pre.data) store_vec<KIND>(row_at<KIND>(e.pre, row) + (size_t)c * (kVec * kWidth<KIND>), pack<KIND>(v), valid);
     if (e.codes.data) {
-        uint32_t top = 0;
-        #pragma unroll
-        for (int i = 0; i < kVec; ++i) top = max(top, i < valid ? magnitude(v[i]) : 0u);
-        const Coding code = coding_of(max_of_8(top));
-        u32x2 q{};
-        #pragma unroll
-        for (int i = 0; i < kVec; ++i) q[i / 4] |= code_of(v[i], code) << (i % 4 * 8);
+        float most = 0.f;
+        if (valid >= kVec) {
+            #pragma unroll
+            for (int i = 0; i < kVec; ++i) most = __builtin_elementwise_maximum(most, __builtin_fabsf(v[i]));
+        } else {
+            #pragma unroll
+            for (int i = 0; i < kVec; ++i) most = i < valid ? __builtin_elementwise_maximum(most, __builtin_fabsf(v[i])) : most;
+        }
+        const Coding code = coding_of(max_of_8(__builtin_bit_cast(uint32_t, most) & 0x7FFFFFFFu));
+        const u32x2 q = {codes_of(v, code), codes_of(v + 4, code)};
         char* const to = (char*)e.codes.data + row * e.codes.stride + (size_t)c * kVec;
         if (valid >= kVec) *(u32x2_a1*)to = q;
         else
