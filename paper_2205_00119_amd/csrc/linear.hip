@@ -234,11 +234,15 @@ __device__ __forceinline__ Unit unit_at(const ProductArgs& g, unsigned i)
     return {g.whole + at, first, min(g.p.k, first + g.depth), g.p.parts + ((size_t)at * g.splits + split) * (g.bm * g.bn)};
 }
 
-constexpr int kStagePitch = 64 + 4;            // floats of a row of a wavefront's results in the LDS
 
 // One workgroup for a tile of BM x BN results, WM x WN wavefronts with 64 columns each.
-// WAY kDirect: whole chunks begin on 16 bytes, so tiles of k go straight into the LDS, two of them in flight; while a wavefront
-// multiplies one half of a tile it reads the next half.
+// WAY kDirect: whole chunks begin on 16 bytes, so tiles of k go straight into the LDS, the next one and the one behind it on their
+// way; while a wavefront multiplies one half of a tile it reads the next half.  Reads and loads are spread among the matrix
+// instructions (us, in front of them / spread: 4096 x 8192 x 4096 bf16 210 / 194, input gradient 4096 x 20480 x 5120 725 / 678, weight
+// gradient 8192 x 4096 x 16384 930 / 851).  Neither the LDS (its ports are busy a quarter of the time, 1 % of that with conflicts) nor
+// memory bounds it: the matrix units are busy 63 to 70 % of the time, the rest goes to the barrier of each tile.  Slower were tiles of 64
+// bytes of k in a ring of four, which wait less for loads and more for barriers (830 / 915 at 8192 x 8192 x 8192), instructions of
+// 32 x 32 (830 / 919), and four wavefronts of 128 x 128 (823 / 887).
 // kThrough: chunks begin on any element; a tile waits in registers while the one before is multiplied.
 // kGuarded: rows shorter than a chunk, tiles of more than 2^31 bytes; every chunk is looked at.  So is the last part of a tile of k
 // in the other two.
@@ -247,8 +251,10 @@ template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN, int WAY>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
 {
     constexpr int kLanes = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, kOut = TM < 4 ? TM : 4;
-    static_assert(TN == 4, "a wavefront's columns are one block of a checkpoint");
-    constexpr int kTileBytes = (BM + BN) * kRowBytes, kOutBytes = WM * WN * kOut * 16 * kStagePitch * 4;
+    static_assert(TN % 4 == 0, "a wavefront's columns are whole blocks of a checkpoint");
+    constexpr int kTileBytes = (BM + BN) * kRowBytes;
+    // a wavefront's results on their way out: floats from row to row in the LDS, and lanes for a row
+    constexpr int kStagePitch = TN * 16 + 4, kOutBytes = WM * WN * kOut * 16 * kStagePitch * 4, kAcross = TN * 16 / kVec;
     __shared__ __attribute__((aligned(1024))) char lds[std::max(2 * kTileBytes, kOutBytes)];
     typedef Stage<KIND, AT, BM, kLanes> StageA;
     typedef Stage<KIND, BT, BN, kLanes> StageB;
@@ -356,16 +362,40 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
                     __syncthreads();
                 } else {
                 const uint32_t place = (uint32_t)(uintptr_t)tile + wave * 1024;
+                constexpr int kLoads = StageA::kCount + StageB::kCount;
+                // loads I to I + N - 1 of a tile
+                auto some = [&](uint32_t to, auto first_of, auto count) {
+                    each<decltype(count)::value>([&](auto c) {
+                        constexpr int I = decltype(first_of)::value + decltype(c)::value;
+                        if constexpr (I < StageA::kCount) load_to_lds<I * kLanes * 16>(from_a, oa[I], to);
+                        else if constexpr (I < kLoads)
+                            load_to_lds<BM * kRowBytes + (I - StageA::kCount) * kLanes * 16>(from_b, ob[I - StageA::kCount], to);
+                    });
+                };
                 auto load = [&](int at) {
-                    const uint32_t to = place + at * kTileBytes;
-                    each<StageA::kCount>([&](auto c) {
-                        load_to_lds<decltype(c)::value * kLanes * 16>(from_a, oa[decltype(c)::value], to);
-                    });
-                    each<StageB::kCount>([&](auto c) {
-                        load_to_lds<BM * kRowBytes + decltype(c)::value * kLanes * 16>(from_b, ob[decltype(c)::value], to);
-                    });
+                    some(place + at * kTileBytes, std::integral_constant<int, 0>{}, std::integral_constant<int, kLoads>{});
                     from_a += step_a;
                     from_b += step_b;
+                };
+                // Half a tile: row by row of results the products of what has been read, what is multiplied next, and with LOADS a part of
+                // the loads of another tile, so that none of them comes in one piece.
+                auto half_of = [&](const PieceA& pa, const PieceB& pb, PieceA& na, PieceB& nb, int at, auto half, auto loads) {
+                    const Reader<KIND, AT, BM> a(tile + at * kTileBytes, wm * TM * 16);
+                    const Reader<KIND, BT, BN> b(tile + at * kTileBytes + BM * kRowBytes, wn * TN * 16);
+                    const uint32_t to = place + (at ^ 1) * kTileBytes;
+                    each<TM>([&](auto r) {
+                        constexpr int M = decltype(r)::value, share = (kLoads + TM - 1) / TM;
+                        if constexpr (M < TN) nb[M] = b.read(M, decltype(half)::value);
+                        na[M] = a.read(M, decltype(half)::value);
+                        if constexpr (decltype(loads)::value) some(to, std::integral_constant<int, M * share>{}, std::integral_constant<int, share>{});
+                        #pragma unroll
+                        for (int n = 0; n < TN; ++n) multiply<KIND>(acc[M][n], pa[M], pb[n]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+                    if constexpr (decltype(loads)::value) {
+                        from_a += step_a;
+                        from_b += step_b;
+                    }
                 };
                 PieceA a0, a1;
                 PieceB b0, b1;
@@ -374,17 +404,16 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
                 landed();
                 read(a0, b0, 0, 0);
                 int at = 0;
-                for (size_t k = whole; k; --k, at ^= 1) {
-                    read(a1, b1, at, 1);
-                    __builtin_amdgcn_sched_barrier(0);          // reads are issued before the products that they pass by
-                    add(a0, b0);
-                    __builtin_amdgcn_sched_barrier(0);
+                size_t k = whole;
+                for (; k > 2; --k, at ^= 1) {                   // the tile behind the next one takes this one's place
+                    half_of(a0, b0, a1, b1, at, std::integral_constant<int, 1>{}, std::false_type{});
                     landed();
-                    if (k > 2) load(at);
-                    read(a0, b0, at ^ 1, 0);                    // behind the last tile: what nothing uses
-                    __builtin_amdgcn_sched_barrier(0);
-                    add(a1, b1);
-                    __builtin_amdgcn_sched_barrier(0);
+                    half_of(a1, b1, a0, b0, at ^ 1, std::integral_constant<int, 0>{}, std::true_type{});
+                }
+                for (; k; --k, at ^= 1) {                       // behind the last tile is read what nothing uses
+                    half_of(a0, b0, a1, b1, at, std::integral_constant<int, 1>{}, std::false_type{});
+                    landed();
+                    half_of(a1, b1, a0, b0, at ^ 1, std::integral_constant<int, 0>{}, std::false_type{});
                 }
                 }
             }
@@ -409,7 +438,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
                 if (more) put(ra, rb, at ^ 1);
             }
         }
-        // A wavefront's results pass through the LDS into rows of 64 columns, eight to a lane.
+        // A wavefront's results pass through the LDS into rows of its columns, eight to a lane.
         typedef __attribute__((address_space(3))) f32x4 lds_f4;
         lds_char* const mine = tile + wave * kOut * 16 * kStagePitch * 4;
         __syncthreads();
@@ -422,10 +451,10 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
                     *(lds_f4*)(mine + ((m * 16 + lane % 16) * kStagePitch + n * 16 + lane / 16 * 4) * 4) = acc[part * kOut + m][n];
             }
             // its own LDS accesses are in order
-            for (int r = lane / 8; r < kOut * 16; r += 8) {
-                const size_t row = m0 + wm * TM * 16 + part * kOut * 16 + r, col = n0 + wn * TN * 16 + lane % 8 * kVec;
+            for (int r = lane / kAcross; r < kOut * 16; r += 64 / kAcross) {
+                const size_t row = m0 + wm * TM * 16 + part * kOut * 16 + r, col = n0 + wn * TN * 16 + lane % kAcross * kVec;
                 if (row >= p.m) break;
-                const lds_char* const from = mine + (r * kStagePitch + lane % 8 * kVec) * 4;
+                const lds_char* const from = mine + (r * kStagePitch + lane % kAcross * kVec) * 4;
                 const f32x4 low = *(const lds_f4*)from, high = *(const lds_f4*)(from + 16);
                 float v[kVec] = {low.x, low.y, low.z, low.w, high.x, high.y, high.z, high.w};
                 const int valid = col < p.n ? (int)min(p.n - col, (size_t)kVec) : 0;

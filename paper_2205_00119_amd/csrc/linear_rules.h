@@ -35,7 +35,7 @@ constexpr size_t copy_stride(size_t row, size_t width) { return ceil_div(row * w
 
 // What a cut into tiles of `tile` rows and columns takes in ns, with the best number of parts for the tiles of the last round.
 // slow: what a tile of k takes against operands on 16 bytes.  Measured (us): a tile of k for all workgroups that fit, 256 x 256, one on
-// a compute unit, 1.6 (4096 x 8192 x 4096 bf16 208), 128 x 128, two on one, 0.93 (8192 x 8192 x 8192 961), one on one 0.57
+// a compute unit, 1.55 (4096 x 8192 x 4096 bf16 194 to 206), 128 x 128, two on one, 0.93 (8192 x 8192 x 8192 961), one on one 0.57
 // (4096 x 8192 x 1024 78); 336 tiles of 128 x 128 with k = 5120 65, in three parts each 71, 160 of 256 x 256 with k = 2560 71;
 // beginning and end of a tile 8 and 4.
 struct TileCost {
@@ -47,7 +47,7 @@ inline TileCost cost_of_tiles(const ProductShape& s, size_t tile, size_t room, d
     const size_t tiles = ceil_div(s.m, tile) * ceil_div(s.n, tile), depths = ceil_div(s.k, 128 / s.width);
     if (s.width == 4) slow *= 8;                           // the rates of the matrix instructions
     const bool large = tile == 256;
-    const double full = (large ? 1600 : 930) * slow, half = (large ? 1600 : 570) * slow, ends = large ? 8000 : 4000;
+    const double full = (large ? 1550 : 930) * slow, half = (large ? 1550 : 570) * slow, ends = large ? 8000 : 4000;
     const size_t slots = large ? kCUs : 2 * kCUs;
     auto rounds = [&](size_t units, size_t depth) {
         const size_t rest = units % slots;
