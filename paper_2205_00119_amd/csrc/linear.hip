@@ -438,9 +438,17 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
                 if (more) put(ra, rb, at ^ 1);
             }
         }
-        // A wavefront's results pass through the LDS into rows of its columns, eight to a lane.
+        // A wavefront's results pass through the LDS into rows of its columns, eight to a lane, whose bias is loaded once.
         typedef __attribute__((address_space(3))) f32x4 lds_f4;
+        constexpr int kStep = 64 / kAcross;                     // rows at a time
         lds_char* const mine = tile + wave * kOut * 16 * kStagePitch * 4;
+        const size_t col = n0 + wn * TN * 16 + lane % kAcross * kVec;
+        const int valid = col < p.n ? (int)min(p.n - col, (size_t)kVec) : 0;
+        Epilogue e = p.e;
+        float bias[kVec] = {};
+        if (e.bias && !unit.parts) load_any((const char*)e.bias, e.param, (unsigned)(col / kVec), valid, bias);
+        const bool bare = !unit.parts && !e.bias && !e.pre.data && !e.codes.data && !e.residual.data && !e.act && e.out_kind == KIND;
+        e.bias = nullptr;
         __syncthreads();
         #pragma unroll
         for (int part = 0; part < TM / kOut; ++part) {
@@ -451,15 +459,38 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
                     *(lds_f4*)(mine + ((m * 16 + lane % 16) * kStagePitch + n * 16 + lane / 16 * 4) * 4) = acc[part * kOut + m][n];
             }
             // its own LDS accesses are in order
-            for (int r = lane / kAcross; r < kOut * 16; r += 64 / kAcross) {
-                const size_t row = m0 + wm * TM * 16 + part * kOut * 16 + r, col = n0 + wn * TN * 16 + lane % kAcross * kVec;
-                if (row >= p.m) break;
-                const lds_char* const from = mine + (r * kStagePitch + lane % kAcross * kVec) * 4;
+            const size_t row0 = m0 + wm * TM * 16 + part * kOut * 16 + lane / kAcross;
+            const int rows = row0 < p.m ? (int)min((p.m - row0 + kStep - 1) / kStep, (size_t)(kOut * 16 / kStep)) : 0;
+            const lds_char* from = mine + (lane / kAcross * kStagePitch + lane % kAcross * kVec) * 4;
+            auto take = [&](float (&v)[kVec]) {
                 const f32x4 low = *(const lds_f4*)from, high = *(const lds_f4*)(from + 16);
-                float v[kVec] = {low.x, low.y, low.z, low.w, high.x, high.y, high.z, high.w};
-                const int valid = col < p.n ? (int)min(p.n - col, (size_t)kVec) : 0;
-                if (unit.parts) store_vec<kF32>((char*)(unit.parts + (row - m0) * BN + (col - n0)), pack<kF32>(v), kVec);
-                else finish<KIND>(p.e, row, (unsigned)(col / kVec), (unsigned)p.n, valid, v);
+                from += kStep * kStagePitch * 4;
+                #pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = low[i];
+                    v[i + 4] = high[i];
+                }
+            };
+            float v[kVec];
+            if (unit.parts) {
+                float* to = unit.parts + (row0 - m0) * BN + (col - n0);
+                for (int r = 0; r < rows; ++r, to += kStep * BN) {
+                    take(v);
+                    store_vec<kF32>((char*)to, pack<kF32>(v), kVec);
+                }
+            } else if (bare) {
+                char* to = (char*)e.out.data + (row0 * e.out.stride + col) * kWidth<KIND>;
+                for (int r = 0; r < rows; ++r, to += e.out.stride * (kStep * kWidth<KIND>)) {
+                    take(v);
+                    store_vec<KIND>(to, pack<KIND>(v), valid);
+                }
+            } else {
+                for (int r = 0; r < rows; ++r) {
+                    take(v);
+                    #pragma unroll
+                    for (int i = 0; i < kVec; ++i) v[i] += bias[i];
+                    finish<KIND>(e, row0 + r * kStep, (unsigned)(col / kVec), (unsigned)p.n, valid, v);
+                }
             }
         }
         __syncthreads();
