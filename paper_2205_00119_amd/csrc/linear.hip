@@ -657,12 +657,12 @@ template <int KIND, bool BT> int launch_few(const ProductArgs& g, void* stream)
     return g.bm == 16 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 2>{});
 }
 
-// Operands copied into rows on 16 bytes, chunk by chunk; blockIdx.y: which.  What is behind a row's end stays as it is.
+// Operands copied into rows on 16 bytes, chunk by chunk; blockIdx.y: which.  Behind the rows and their ends are zeros.
 struct Copy {
     const char* from;
     char* to;
-    size_t rows, stride, chunks;               // bytes from row to row of the operand; chunks of a row of the copy
-    unsigned bytes;                            // of a row
+    size_t there, rows, stride, chunks;        // rows of the operand, of the copy; bytes from one to the next; chunks of the copy's
+    size_t bytes;                              // of the operand's
 };
 struct CopyArgs {
     Copy c[2];
@@ -677,8 +677,8 @@ template <int KIND> __global__ __launch_bounds__(kCopyLanes) void copy_kernel(Co
         const unsigned at = (unsigned)(base - row0 * c.chunks) + threadIdx.x, chunks = (unsigned)c.chunks, up = at / chunks;
         const size_t row = row0 + up, i = base + threadIdx.x;
         if (i >= all) break;
-        const unsigned place = (at - up * chunks) * 16;
-        const u32x4 q = load_chunk<KIND>(c.from + row * c.stride + place, (ptrdiff_t)((c.bytes - place) / kWidth<KIND>));
+        const ptrdiff_t place = (ptrdiff_t)(at - up * chunks) * 16, valid = row < c.there ? ((ptrdiff_t)c.bytes - place) / (ptrdiff_t)kWidth<KIND> : 0;
+        const u32x4 q = load_chunk<KIND>(c.from + row * c.stride + place, valid);
         *(u32x4*)(c.to + i * 16) = q;
     }
 }
@@ -701,10 +701,12 @@ int launch_product(const Product& p, const ProductPlan& plan, int kind, void* st
         CopyArgs c{};
         size_t most = 0;
         int n = 0;
+        if (plan.a_copy && plan.b_copy) g.p.k = copy_k(p.k, width);
         auto take = [&](ConstRows& m, bool turned, size_t& rows, size_t bytes) {
             if (!bytes) return;
-            const size_t high = turned ? p.k : rows, wide = turned ? rows : p.k, stride = copy_stride(wide, width);
-            c.c[n++] = {(const char*)m.data, to, high, m.stride * width, stride * width / 16, (unsigned)(wide * width)};
+            const size_t there = turned ? p.k : rows, high = turned ? g.p.k : rows, wide = turned ? rows : p.k;
+            const size_t stride = copy_stride(turned ? rows : g.p.k, width);
+            c.c[n++] = {(const char*)m.data, to, there, high, m.stride * width, stride * width / 16, wide * width};
             most = std::max(most, bytes / 16);
             m = {to, stride};
             if (turned) rows = stride;

@@ -30,6 +30,8 @@ struct ProductPlan {
 constexpr size_t parts_bytes(const ProductPlan& p) { return p.splits > 1 ? p.shared * p.splits * p.bm * p.bn * 4 : 0; }
 // Parts, copies, and what the first copy's place on 16 bytes may take.
 constexpr size_t workspace_of(const ProductPlan& p) { return parts_bytes(p) + (p.a_copy + p.b_copy ? p.a_copy + p.b_copy + 16 : 0); }
+// k of operands that are both copied: zeros fill it up to whole tiles.
+constexpr size_t copy_k(size_t k, size_t width) { return ceil_div(k * width, 128) * 128 / width; }
 // Elements of a row of a copy.
 constexpr size_t copy_stride(size_t row, size_t width) { return ceil_div(row * width, 16) * 16 / width; }
 
@@ -99,8 +101,9 @@ inline ProductPlan plan_product(const ProductShape& s)
     // 111 / 81, so 1.8 times as long, which 128 x 128 never is;
     // 1000 x 1001 x 1003 in two parts 20 / 25.  32-bit products are bound by the matrix instructions.
     const TileCost own = s.width == 4 ? best(kLinearWorkspace, 1.05, 0) : best(kLinearWorkspace, 1.5, s.a_turned ? 0 : 1.3);
-    const size_t a = s.a_on_16 ? 0 : (s.a_turned ? s.k * copy_stride(s.m, s.width) : s.m * copy_stride(s.k, s.width)) * s.width;
-    const size_t b = s.b_on_16 ? 0 : (s.b_turned ? s.k * copy_stride(s.n, s.width) : s.n * copy_stride(s.k, s.width)) * s.width;
+    const size_t k = s.a_on_16 || s.b_on_16 ? s.k : copy_k(s.k, s.width);
+    const size_t a = s.a_on_16 ? 0 : (s.a_turned ? k * copy_stride(s.m, s.width) : s.m * copy_stride(k, s.width)) * s.width;
+    const size_t b = s.b_on_16 ? 0 : (s.b_turned ? k * copy_stride(s.n, s.width) : s.n * copy_stride(k, s.width)) * s.width;
     if (a > kLinearWorkspace || b > kLinearWorkspace || a + b + 16 > kLinearWorkspace) return own.plan;
     TileCost copied = best(kLinearWorkspace - a - b - 16, 1, 1);
     copied.ns += (a + b) / 2700.0 + 4500;

@@ -57,7 +57,8 @@ def test_every_tile_and_every_k_is_taken_once(plan):
         copied = [p["a_copy"], p["b_copy"]]
         assert (not copied[0] or not a16) and (not copied[1] or not b16) and (chunks or copied == [0, 0]), what
         if any(copied):                                                                # all that is off 16 bytes
-            rows = [(k, m) if turned[0] else (m, k), (k, n) if turned[1] else (n, k)]
+            kp = k if a16 or b16 else depths * 128 // width
+            rows = [(kp, m) if turned[0] else (m, kp), (kp, n) if turned[1] else (n, kp)]
             for bytes_, on, (r, c) in zip(copied, (a16, b16), rows):
                 assert bytes_ == (0 if on else r * ceil(c * width, 16) * 16), what
 
