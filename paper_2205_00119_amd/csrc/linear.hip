@@ -48,6 +48,27 @@ template <int KIND> __device__ __forceinline__ u32x4 load_chunk(const char* p, p
     }
 }
 
+// The chunk's elements from `by` on, less than a chunk has, come to its front; zeros follow.
+template <int KIND> __device__ __forceinline__ void move_up(u32x4& q, int by)
+{
+    #pragma unroll
+    for (int step = 2; step; step /= 2) {
+        const bool go = by & (KIND == kF32 ? step : 2 * step);
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t from = i + step < 4 ? q[i + step < 4 ? i + step : 3] : 0u, own = q[i];
+            q[i] = go ? from : own;
+        }
+    }
+    if constexpr (KIND != kF32) {
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t next = i < 3 ? q[i < 3 ? i + 1 : 3] : 0u, own = q[i];
+            q[i] = by & 1 ? own >> 16 | next << 16 : own;
+        }
+    }
+}
+
 // How the lanes of a workgroup bring a tile of ROWS rows into the LDS: chunk i * LANES + lane in the order of the places there.
 template <int KIND, bool TURNED, int ROWS, int LANES> struct Stage {
     static constexpr int kCount = ROWS * 8 / LANES, kAcross = ROWS * (int)kWidth<KIND> / 16;
@@ -86,6 +107,20 @@ template <int KIND, bool TURNED, int ROWS, int LANES> struct Stage {
         const uint32_t step = (uint32_t)stride, d = depth(i);
         return (TURNED ? d * step + r : r * step + d) * (uint32_t)kWidth<KIND>;
     }
+    // Chunk i of the last part of a tile of k, which begins at k0 and ends at `last`, loaded without a branch: from a place inside, and
+    // moved up and cleared by settle().
+    static __device__ __forceinline__ u32x4 rest(const ConstRows& m, size_t row0, size_t k0, size_t rows, size_t last, int i)
+    {
+        const size_t k = min(k0 + depth(i), last - (TURNED ? 1 : kChunk<KIND>));
+        const size_t at = TURNED ? k * m.stride + row0 + row(i) - early(rows, i) : (row0 + min((size_t)row(i), rows - 1)) * m.stride + k;
+        return *(const u32x4_a2*)((const char*)m.data + at * kWidth<KIND>);
+    }
+    static __device__ __forceinline__ void settle(u32x4& q, size_t k0, size_t rows, size_t last, int i)
+    {
+        const ptrdiff_t behind = (ptrdiff_t)(k0 + depth(i)) - (ptrdiff_t)last;      // of its first k; 0 and more: nothing is there
+        move_up<KIND>(q, TURNED ? early(rows, i) & (kChunk<KIND> - 1) : (int)max(behind + kChunk<KIND>, (ptrdiff_t)0) & (kChunk<KIND> - 1));
+        if (behind >= 0) q = u32x4{};
+    }
     static __device__ __forceinline__ const char* first(const ConstRows& m, size_t row0, size_t k0, size_t rows)
     {
         return (const char*)m.data + (TURNED ? k0 * m.stride + row0 - lower(rows) : row0 * m.stride + k0) * kWidth<KIND>;
@@ -98,26 +133,6 @@ template <int KIND, bool TURNED, int ROWS, int LANES> struct Stage {
 template <int TO> __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t to)
 {
     asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(base), "v"(offset), "s"(to), "i"(TO) : "memory", "scc");
-}
-// The chunk's elements from `by` on come to its front.
-template <int KIND> __device__ __forceinline__ void move_up(u32x4& q, int by)
-{
-    #pragma unroll
-    for (int step = 2; step; step /= 2) {
-        const bool go = by & (KIND == kF32 ? step : 2 * step);
-        #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t from = q[i + step < 4 ? i + step : 3];
-            q[i] = go ? from : q[i];
-        }
-    }
-    if constexpr (KIND != kF32) {
-        #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t next = q[i < 3 ? i + 1 : 3], own = q[i];
-            q[i] = by & 1 ? own >> 16 | next << 16 : own;
-        }
-    }
 }
 // f(std::integral_constant<int, i>) for every i below N.
 template <int... I, typename F> __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f)
@@ -244,11 +259,11 @@ __device__ __forceinline__ Unit unit_at(const ProductArgs& g, unsigned i)
 // bytes of k in a ring of four, which wait less for loads and more for barriers (830 / 915 at 8192 x 8192 x 8192), instructions of
 // 32 x 32 (830 / 919), and four wavefronts of 128 x 128 (823 / 887).
 // kThrough: chunks begin on any element; a tile waits in registers while the one before is multiplied.
-// kGuarded: rows shorter than a chunk, tiles of more than 2^31 bytes; every chunk is looked at.  So is the last part of a tile of k
-// in the other two.
+// kGuarded: rows shorter than a chunk, tiles of more than 2^31 bytes; every chunk is looked at.
+
 enum { kDirect, kThrough, kGuarded };
 template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN, int WAY>
-__global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
+__global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 : 1) void product_kernel(ProductArgs g)
 {
     constexpr int kLanes = 64 * WM * WN, TM = BM / WM / 16, TN = BN / WN / 16, kOut = TM < 4 ? TM : 4;
     static_assert(TN % 4 == 0, "a wavefront's columns are whole blocks of a checkpoint");
@@ -302,7 +317,14 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
         if constexpr (WAY != kGuarded) {
             if (const size_t rest = last > first ? (last - first) % kDepth<KIND> : 0) {      // in front: a sum has no order
                 u32x4 ra[StageA::kCount], rb[StageB::kCount];
-                fetch(ra, rb, last - rest);
+                #pragma unroll
+                for (int c = 0; c < StageA::kCount; ++c) ra[c] = StageA::rest(p.a, m0, last - rest, g.a_rows - m0, last, c);
+                #pragma unroll
+                for (int c = 0; c < StageB::kCount; ++c) rb[c] = StageB::rest(p.b, n0, last - rest, g.b_rows - n0, last, c);
+                #pragma unroll
+                for (int c = 0; c < StageA::kCount; ++c) StageA::settle(ra[c], last - rest, g.a_rows - m0, last, c);
+                #pragma unroll
+                for (int c = 0; c < StageB::kCount; ++c) StageB::settle(rb[c], last - rest, g.b_rows - n0, last, c);
                 put(ra, rb, 0);
                 __syncthreads();
                 #pragma unroll
@@ -503,6 +525,10 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs g)
 //   b not turned   16 columns to an instruction, lane i of 16 has chunk lane / 16 of row i;
 //   b turned       a lane has a chunk of columns of kChunk k, which it turns around in registers: instruction j takes column j of
 //                  every chunk.
+// us, in tiles of 128 rows / so: 1 x 2560 x 10240 bf16 16.6 / 12.1 (the weights alone take 7.8, a launch 4), 1 x 10240 x 2560 22.3 / 14.5,
+// 16 x 2560 x 10240 f32 63.7 / 31.3, its input's gradient 65.8 / 22.4; 8 x 5120 x 20480 36.4 / 39.4, where tiles have enough to do.
+// Rows of b off 16 bytes are left to the tiles unless b is turned: 16 rows at a time from 64 bytes each, 56 / 150.  Two tiles of k at a
+// time and 32 or 64 columns were slower (39 / 51).
 constexpr int kFewWaves = 8;
 template <int KIND, bool BT, int TM, int BN>
 __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(ProductArgs g)
@@ -618,7 +644,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_rows_kernel(ProductArgs g)
     }
 }
 
-// The sums of the shared tiles' parts, in ascending order, and what happens to them.
+// The sums of the shared tiles' parts, in ascending order, and what happens to them: 3.9 us for few parts, which is the launch.
 constexpr int kJoinLanes = 64;
 template <int KIND> __global__ __launch_bounds__(kJoinLanes) void join_kernel(ProductArgs g)
 {
@@ -657,7 +683,8 @@ template <int KIND, bool BT> int launch_few(const ProductArgs& g, void* stream)
     return g.bm == 16 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 2>{});
 }
 
-// Operands copied into rows on 16 bytes, chunk by chunk; blockIdx.y: which.  Behind the rows and their ends are zeros.
+// Operands copied into rows on 16 bytes, chunk by chunk; blockIdx.y: which.  Behind the rows and their ends are zeros, so that no tile
+// of k is in part (2047 x 5121 x 2561 binary16 103 / 78 us).  47 MB take 16 us, 5.9 TB/s read and written.
 struct Copy {
     const char* from;
     char* to;

@@ -37,9 +37,8 @@ constexpr size_t copy_stride(size_t row, size_t width) { return ceil_div(row * w
 
 // What a cut into tiles of `tile` rows and columns takes in ns, with the best number of parts for the tiles of the last round.
 // slow: what a tile of k takes against operands on 16 bytes.  Measured (us): a tile of k for all workgroups that fit, 256 x 256, one on
-// a compute unit, 1.55 (4096 x 8192 x 4096 bf16 194 to 206), 128 x 128, two on one, 0.93 (8192 x 8192 x 8192 961), one on one 0.57
-// (4096 x 8192 x 1024 78); 336 tiles of 128 x 128 with k = 5120 65, in three parts each 71, 160 of 256 x 256 with k = 2560 71;
-// beginning and end of a tile 8 and 4.
+// a compute unit, 1.45 (4096 x 8192 x 4096 bf16 191), 128 x 128, two on one, 0.9 (2048 x 4096 x 4096 62.5), one on one 0.56
+// (4096 x 8192 x 1024 78); 320 tiles of 128 x 128 with k = 5120 63.5, in three parts each 71; beginning and end of a tile 5 and 3.5.
 struct TileCost {
     ProductPlan plan;
     double ns;
@@ -49,7 +48,7 @@ inline TileCost cost_of_tiles(const ProductShape& s, size_t tile, size_t room, d
     const size_t tiles = ceil_div(s.m, tile) * ceil_div(s.n, tile), depths = ceil_div(s.k, 128 / s.width);
     if (s.width == 4) slow *= 8;                           // the rates of the matrix instructions
     const bool large = tile == 256;
-    const double full = (large ? 1550 : 930) * slow, half = (large ? 1550 : 570) * slow, ends = large ? 8000 : 4000;
+    const double full = (large ? 1450 : 900) * slow, half = (large ? 1450 : 560) * slow, ends = large ? 5000 : 3500;
     const size_t slots = large ? kCUs : 2 * kCUs;
     auto rounds = [&](size_t units, size_t depth) {
         const size_t rest = units % slots;
@@ -65,7 +64,7 @@ inline TileCost cost_of_tiles(const ProductShape& s, size_t tile, size_t room, d
             if (units > 2 * slots || units * tile * tile * 4 > room) break;
             if (ceil_div(depths, depth) < splits) continue;
             // the parts are written and read, and a second launch
-            const double ns = rounds(tiles - shared, depths) + rounds(units, depth) + units * tile * tile * 8 / 5000.0 + 4000;
+            const double ns = rounds(tiles - shared, depths) + rounds(units, depth) + units * tile * tile * 8 / 5000.0 + 5000;
             if (ns < best.ns) best = {{false, tile, tile, tiles - shared, shared, splits, depth, 0, 0}, ns};
         }
     }
@@ -96,17 +95,17 @@ inline ProductPlan plan_product(const ProductShape& s)
     };
     const bool off = s.chunks && !(s.a_on_16 && s.b_on_16);
     if (!off) return best(kLinearWorkspace, 1, 1).plan;
-    // Loads off 16 bytes take the L1 cache twice the time and more.  us, binary16, so / copied first: 128 x 128, 2047 x 5121 x 2561
-    // 131 / 104, its gradients 119 / 105 and 111 / 90; 256 x 256, 4095 x 3001 x 3003 bf16 113 / 104, the weight's gradient above
-    // 111 / 81, so 1.8 times as long, which 128 x 128 never is;
-    // 1000 x 1001 x 1003 in two parts 20 / 25.  32-bit products are bound by the matrix instructions.
-    const TileCost own = s.width == 4 ? best(kLinearWorkspace, 1.05, 0) : best(kLinearWorkspace, 1.5, s.a_turned ? 0 : 1.3);
+    // Loads off 16 bytes take the L1 cache twice the time and more.  us, so / copied first: 128 x 128, 2047 x 5121 x 2561 133 / 92, its
+    // gradients 107 / 86 and 103 / 80, 300 x 2047 x 5121 36.2 / 35.9; 256 x 256, 4095 x 3001 x 3003 107 / 83, 4095 x 8193 x 4095 256 / 254.
+    // Both turned, 256 x 256 takes 1.8 times as long as on 16 bytes, and 128 x 128 is faster.  32-bit products are bound by the matrix
+    // instructions.
+    const TileCost own = s.width == 4 ? best(kLinearWorkspace, 1.05, 0) : best(kLinearWorkspace, 1.6, s.a_turned ? 0 : 1.45);
     const size_t k = s.a_on_16 || s.b_on_16 ? s.k : copy_k(s.k, s.width);
     const size_t a = s.a_on_16 ? 0 : (s.a_turned ? k * copy_stride(s.m, s.width) : s.m * copy_stride(k, s.width)) * s.width;
     const size_t b = s.b_on_16 ? 0 : (s.b_turned ? k * copy_stride(s.n, s.width) : s.n * copy_stride(k, s.width)) * s.width;
     if (a > kLinearWorkspace || b > kLinearWorkspace || a + b + 16 > kLinearWorkspace) return own.plan;
     TileCost copied = best(kLinearWorkspace - a - b - 16, 1, 1);
-    copied.ns += (a + b) / 2700.0 + 4500;
+    copied.ns += (a + b) / 3000.0 + 4000;
     if (copied.ns >= own.ns) return own.plan;
     copied.plan.a_copy = a;
     copied.plan.b_copy = b;

@@ -322,3 +322,77 @@ def test_far_values_of_activations():
             far = np.abs(z32) > 100
             s = np.where(far & (act != "none"), (z32 > 0).astype(float), ref.slope(np.where(far, 0, z32), act)[0])
         assert np.abs(dx.f64() - s).max() < 2e-6, act
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(8, 2048, 640), (300, 1100, 650), (64, 4096, 512), (1, 4000, 24)])
+def test_results_in_the_place_of_what_is_added(rows, cin, cout):
+    """Also where a second launch joins parts."""
+    r = np.random.default_rng(rows)
+    x, w = Matrix(rows, cin, "bf16", data=r.normal(0, 1, (rows, cin))), Matrix(cout, cin, "bf16", data=r.normal(0, cin ** -0.5, (cout, cin)))
+    ws, work = linear_scratch(rows, cin, cout)
+    data = r.normal(0, 1, (rows, cout))
+    out, res = Matrix(rows, cout, "bf16"), Matrix(rows, cout, "bf16", data=data)
+    key = dict(act=ACT["gelu"], dtype=CODE["bf16"], param_dtype=CODE["bf16"])
+    mics.mics_linear(out.t, None, None, None, x.t, w.t, None, res.t, rows, cin, cout, **key, **work)
+    mics.mics_linear(res.t, None, None, None, x.t, w.t, None, res.t, rows, cin, cout, **key, **work)
+    assert torch.equal(out.t, res.t)
+    dz, d1, d2 = Matrix(rows, cout, "bf16", data=data), Matrix(rows, cin, "bf16"), Matrix(rows, cin, "bf16", data=r.normal(0, 1, (rows, cin)))
+    mics.mics_linear_backward_input(d1.t, dz.t, w.t, d2.t, rows, cin, cout, dtype=CODE["bf16"], **work)
+    mics.mics_linear_backward_input(d2.t, dz.t, w.t, d2.t, rows, cin, cout, dtype=CODE["bf16"], **work)
+    assert torch.equal(d1.t, d2.t)
+
+
+@pytest.mark.parametrize("fmt,far", [("bf16", 1 << 22), ("f32", 1 << 21)])
+def test_rows_too_far_apart_for_32_bit_offsets(fmt, far):
+    rows, cin, cout = 3, 40, 24
+    r = np.random.default_rng(1)
+    x, w, dz = (Matrix(n, m, fmt, far, 0, whole_numbers(r, n, m, 8)) for n, m in ((rows, cin), (cout, cin), (rows, cout)))
+    ws, work = linear_scratch(rows, cin, cout)
+    out, dx, dw = Matrix(rows, cout, fmt), Matrix(rows, cin, fmt), Matrix(cout, cin, "f32")
+    mics.mics_linear(out.t, None, None, None, x.t, w.t, None, None, rows, cin, cout, act=0, dtype=CODE[fmt], param_dtype=0,
+                     strides=(cout, cout, cout, x.stride, w.stride, cout), **work)
+    mics.mics_linear_backward_input(dx.t, dz.t, w.t, None, rows, cin, cout, dtype=CODE[fmt], strides=(cin, dz.stride, w.stride, cin), **work)
+    mics.mics_linear_backward_weight(dw.t, dz.t, x.t, rows, cin, cout, dtype=CODE[fmt], grad_dtype=CODE["f32"],
+                                     strides=(cin, dz.stride, x.stride), **work)
+    assert np.array_equal(out.f64(), nearest(x.f64() @ w.f64().T, fmt)) and np.array_equal(dx.f64(), nearest(dz.f64() @ w.f64(), fmt))
+    assert np.array_equal(dw.f64(), dz.f64().T @ x.f64())
+
+
+@pytest.mark.parametrize("fmt,small,large", [("f16", 2.0 ** -20, 2.0 ** 10), ("bf16", 2.0 ** -130, 2.0 ** 100)])
+@pytest.mark.parametrize("rows", [3, 200])
+def test_subnormal_elements_count(fmt, small, large, rows):
+    x, w = Matrix(rows, 64, fmt, data=np.full((rows, 64), small)), Matrix(40, 64, fmt, data=np.full((40, 64), large))
+    out = Matrix(rows, 40, "bf16" if fmt == "bf16" else "f16")
+    ws, work = linear_scratch(rows, 64, 40)
+    assert (x.f64() == small).all()
+    mics.mics_linear(out.t, None, None, None, x.t, w.t, None, None, rows, 64, 40, act=0, dtype=CODE[fmt], param_dtype=0, **work)
+    assert (out.f64() == 64 * small * large).all()
+
+
+def test_nan_behind_the_ends_of_rows_is_not_read_into_sums():
+    """What lies between rows, and rows that belong to others, hold NaN."""
+    for fmt in ("bf16", "f32"):
+        for rows, cin, cout, pad in ((5, 70, 33, 10), (150, 201, 130, 7), (300, 1001, 260, 3)):
+            r = np.random.default_rng(cin)
+            x, w, dz = (Matrix(n, m, fmt, pad, 1, whole_numbers(r, n, m, 4)) for n, m in ((rows, cin), (cout, cin), (rows, cout)))
+            for m in (x, w, dz):
+                keep = m.t.clone()
+                m.whole.fill_(float("nan"))
+                m.t.copy_(keep)
+            ws, work = linear_scratch(rows, cin, cout)
+            out, dx, dw = Matrix(rows, cout, fmt), Matrix(rows, cin, fmt), Matrix(cout, cin, "f32")
+            codes, scales = Matrix(rows, cout, "i8"), Vector(mics.mics_checkpoint_scales(rows, cout), "f32")
+            work["workspace"].fill_(0xFF)
+            mics.mics_linear(out.t, None, codes.t, scales.v, x.t, w.t, None, None, rows, cin, cout, act=0, dtype=CODE[fmt], param_dtype=0,
+                             strides=(cout, cout, cout, x.stride, w.stride, cout), **work)
+            work["workspace"].fill_(0xFF)
+            mics.mics_linear_backward_input(dx.t, dz.t, w.t, None, rows, cin, cout, dtype=CODE[fmt], strides=(cin, dz.stride, w.stride, cin),
+                                            **work)
+            work["workspace"].fill_(0xFF)
+            mics.mics_linear_backward_weight(dw.t, dz.t, x.t, rows, cin, cout, dtype=CODE[fmt], grad_dtype=CODE["f32"],
+                                             strides=(cin, dz.stride, x.stride), **work)
+            z = x.f64() @ w.f64().T
+            assert np.array_equal(out.f64(), nearest(z, fmt)) and np.array_equal(dw.f64(), dz.f64().T @ x.f64())
+            assert np.array_equal(dx.f64(), nearest(dz.f64() @ w.f64(), fmt))
+            want, steps = ref.checkpoint(z.astype(np.float32))
+            assert np.array_equal(codes.t.cpu().numpy(), want) and np.array_equal(scales.f64(), steps.ravel().astype(np.float64))
