@@ -407,7 +407,11 @@ __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 :
                     const uint32_t to = place + (at ^ 1) * kTileBytes;
                     each<TM>([&](auto r) {
                         constexpr int M = decltype(r)::value, share = (kLoads + TM - 1) / TM;
-                        if constexpr (M < TN) nb[M] = b.read(M, decltype(half)::value);
+                        constexpr int columns = (TN + TM - 1) / TM;
+                        each<columns>([&](auto c) {
+                            constexpr int N = M * columns + decltype(c)::value;
+                            if constexpr (N < TN) nb[N] = b.read(N, decltype(half)::value);
+                        });
                         na[M] = a.read(M, decltype(half)::value);
                         if constexpr (decltype(loads)::value) some(to, std::integral_constant<int, M * share>{}, std::integral_constant<int, share>{});
                         #pragma unroll
@@ -759,6 +763,8 @@ int launch_product(const Product& p, const ProductPlan& plan, int kind, void* st
                 return launch_tiles<KIND, AT, BT, 128, 2, 2, kGuarded>(g, stream);
             return dispatch_flag(on_16(g.p.a, AT, g.a_rows, W) && on_16(g.p.b, BT, g.b_rows, W), [&](auto D) {
                 constexpr int WAY = decltype(D)::value ? kDirect : kThrough;
+                if constexpr (KIND == kF32)
+                    if (plan.bm == 64) return launch_tiles<KIND, AT, BT, 64, 4, 1, WAY>(g, stream);
                 if constexpr (KIND != kF32 && !(AT && WAY == kThrough))
                     if (plan.bm == 256) return launch_tiles<KIND, AT, BT, 256, 2, 4, WAY>(g, stream);
                 return launch_tiles<KIND, AT, BT, 128, 2, 2, WAY>(g, stream);

@@ -39,6 +39,8 @@ constexpr size_t copy_stride(size_t row, size_t width) { return ceil_div(row * w
 // slow: what a tile of k takes against operands on 16 bytes.  Measured (us): a tile of k for all workgroups that fit, 256 x 256, one on
 // a compute unit, 1.45 (4096 x 8192 x 4096 bf16 191), 128 x 128, two on one, 0.9 (2048 x 4096 x 4096 62.5), one on one 0.56
 // (4096 x 8192 x 1024 78); 320 tiles of 128 x 128 with k = 5120 63.5, in three parts each 71; beginning and end of a tile 5 and 3.5.
+// In 32 bits, of 128 x 128, two on one 3.66 (2048 x 4096 x 4096 468) and one on one 1.95, of 64 x 64 1.06 and 0.69 (input gradient
+// 154 x 5120 x 5120 in one part 113, in three 92; of 128 x 128 in three 118).
 struct TileCost {
     ProductPlan plan;
     double ns;
@@ -46,14 +48,20 @@ struct TileCost {
 inline TileCost cost_of_tiles(const ProductShape& s, size_t tile, size_t room, double slow)
 {
     const size_t tiles = ceil_div(s.m, tile) * ceil_div(s.n, tile), depths = ceil_div(s.k, 128 / s.width);
-    if (s.width == 4) slow *= 8;                           // the rates of the matrix instructions
     const bool large = tile == 256;
-    const double full = (large ? 1450 : 900) * slow, half = (large ? 1450 : 560) * slow, ends = large ? 5000 : 3500;
+    double full = large ? 1450 : 900, half = large ? 1450 : 560, ends = large ? 5000 : 3500;
     const size_t slots = large ? kCUs : 2 * kCUs;
+    if (s.width == 4) {
+        full = tile == 128 ? 3660 : 1060;
+        half = tile == 128 ? 1950 : 690;
+    }
+    full *= slow;
+    half *= slow;
     auto rounds = [&](size_t units, size_t depth) {
         const size_t rest = units % slots;
         double last = half;
-        if (rest > kCUs) last += (full - half) * (0.3 + 0.7 * (double)(rest - kCUs) / kCUs);
+        // in 32 bits the matrix instructions of a compute unit with two workgroups decide, in 16 what all share does too
+        if (rest > kCUs) last += (full - half) * (s.width == 4 ? 1 : 0.3 + 0.7 * (double)(rest - kCUs) / kCUs);
         return (units / slots) * (depth * full + ends) + (rest ? depth * last + ends : 0);
     };
     TileCost best{{false, tile, tile, tiles, 0, 1, depths, 0, 0}, rounds(tiles, depths)};
@@ -89,7 +97,11 @@ inline ProductPlan plan_product(const ProductShape& s)
     }
     auto best = [&](size_t room, double slow_128, double slow_256) {           // 0: no tiles of 256 x 256
         const TileCost small = cost_of_tiles(s, 128, room, slow_128);
-        if (s.width == 4 || !s.chunks || slow_256 == 0) return small;
+        if (s.width == 4 && s.chunks) {                    // narrower tiles, since idle rows and columns cost as much as others
+            const TileCost tiny = cost_of_tiles(s, 64, room, slow_128);
+            return tiny.ns < small.ns ? tiny : small;
+        }
+        if (!s.chunks || slow_256 == 0) return small;
         const TileCost large = cost_of_tiles(s, 256, room, slow_256);
         return large.ns <= small.ns ? large : small;
     };
