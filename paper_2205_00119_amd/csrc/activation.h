@@ -166,6 +166,8 @@ __device__ __forceinline__ void finish(const Epilogue& e, size_t row, unsigned c
         #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] += t[i];
     }
+    Raw<KIND> residual;                        // loaded before anything is stored: pre may take its place
+    if (e.residual.data) residual = load_vec<KIND>(row_at<KIND>(e.residual, row) + (size_t)c * (kVec * kWidth<KIND>), valid);
     if (e.pre.data) store_vec<KIND>(row_at<KIND>(e.pre, row) + (size_t)c * (kVec * kWidth<KIND>), pack<KIND>(v), valid);
     if (e.codes.data) {
         float most = 0.f;
@@ -190,7 +192,7 @@ __device__ __forceinline__ void finish(const Epilogue& e, size_t row, unsigned c
         for (int i = 0; i < kVec; ++i) v[i] = act_of<decltype(A)::value>(v[i]);
     });
     if (e.residual.data) {
-        unpack<KIND>(load_vec<KIND>(row_at<KIND>(e.residual, row) + (size_t)c * (kVec * kWidth<KIND>), valid), t);
+        unpack<KIND>(residual, t);
         #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] = t[i] + v[i];
     }

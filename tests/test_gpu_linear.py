@@ -342,6 +342,20 @@ def test_results_in_the_place_of_what_is_added(rows, cin, cout):
     assert torch.equal(d1.t, d2.t)
 
 
+@pytest.mark.parametrize("rows,cin,cout", [(8, 2048, 640), (300, 1100, 650), (1, 4000, 24), (129, 64, 131)])
+@pytest.mark.parametrize("fmt", ["bf16", "f32"])
+def test_what_is_kept_in_the_place_of_the_residual(rows, cin, cout, fmt):
+    r = np.random.default_rng(rows)
+    x, w = Matrix(rows, cin, fmt, data=r.normal(0, 1, (rows, cin))), Matrix(cout, cin, fmt, data=r.normal(0, cin ** -0.5, (cout, cin)))
+    ws, work = linear_scratch(rows, cin, cout)
+    out, pre, again = (Matrix(rows, cout, fmt) for _ in range(3))
+    res = Matrix(rows, cout, fmt, data=r.normal(0, 1, (rows, cout)))
+    key = dict(act=ACT["gelu"], dtype=CODE[fmt], param_dtype=0)
+    mics.mics_linear(out.t, pre.t, None, None, x.t, w.t, None, res.t, rows, cin, cout, **key, **work)
+    mics.mics_linear(again.t, res.t, None, None, x.t, w.t, None, res.t, rows, cin, cout, **key, **work)
+    assert torch.equal(out.t, again.t) and torch.equal(pre.t, res.t)
+
+
 @pytest.mark.parametrize("fmt,far", [("bf16", 1 << 22), ("f32", 1 << 21)])
 def test_rows_too_far_apart_for_32_bit_offsets(fmt, far):
     rows, cin, cout = 3, 40, 24
