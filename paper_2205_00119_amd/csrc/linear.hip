@@ -69,25 +69,25 @@ template <int KIND> __device__ __forceinline__ void move_up(u32x4& q, int by)
     }
 }
 
-// How the lanes of a workgroup bring a tile of ROWS rows into the LDS: chunk i * LANES + lane in the order of the places there.
+// How the lanes of a workgroup bring a tile of ROWS rows into the LDS: chunk i * LANES + t in the order of the places there, t: the lane.
 template <int KIND, bool TURNED, int ROWS, int LANES> struct Stage {
     static constexpr int kCount = ROWS * 8 / LANES, kAcross = ROWS * (int)kWidth<KIND> / 16;
     static_assert(ROWS * 8 % LANES == 0, "");
     // row (turned: first of the rows) and k (first of them; turned: the k) of the tile that chunk i holds
-    static __device__ __forceinline__ int row(int i)
+    static __device__ __forceinline__ int row(int t, int i)
     {
-        const int s = i * LANES + (int)threadIdx.x;
+        const int s = i * LANES + t;
         return TURNED ? ((s % kAcross) ^ twist<KIND>(s / kAcross)) * kChunk<KIND> : s / 8;
     }
-    static __device__ __forceinline__ int depth(int i)
+    static __device__ __forceinline__ int depth(int t, int i)
     {
-        const int s = i * LANES + (int)threadIdx.x;
+        const int s = i * LANES + t;
         return TURNED ? s / kAcross : ((s % 8) ^ (s / 8 % 8)) * kChunk<KIND>;
     }
     // Chunk i, whatever lies behind the last of `rows` rows or of `k` from this tile on read as 0.
-    static __device__ __forceinline__ u32x4 load(const ConstRows& m, size_t row0, size_t k0, size_t rows, size_t k, int i)
+    static __device__ __forceinline__ u32x4 load(const ConstRows& m, size_t row0, size_t k0, size_t rows, size_t k, int t, int i)
     {
-        const int r = row(i), d = depth(i);
+        const int r = row(t, i), d = depth(t, i);
         const ptrdiff_t right = (ptrdiff_t)(rows - row0) - r, deep = (ptrdiff_t)(k - k0) - d;
         const size_t at = TURNED ? (k0 + d) * m.stride + row0 + r : (row0 + r) * m.stride + k0 + d;
         return load_chunk<KIND>((const char*)m.data + at * kWidth<KIND>, right <= 0 || deep <= 0 ? 0 : TURNED ? right : deep);
@@ -97,28 +97,28 @@ template <int KIND, bool TURNED, int ROWS, int LANES> struct Stage {
     // with them, and is moved up in registers; where that is in front of the tile, the address is that much lower.
     static __device__ __forceinline__ int lower(size_t rows) { return TURNED ? max(kChunk<KIND> - (int)min(rows, (size_t)ROWS), 0) : 0; }
     // What chunk i is moved up by.
-    static __device__ __forceinline__ int early(size_t rows, int i)
+    static __device__ __forceinline__ int early(size_t rows, int t, int i)
     {
-        return max(row(i) - ((int)min(rows, (size_t)ROWS) - kChunk<KIND>), 0);
+        return max(row(t, i) - ((int)min(rows, (size_t)ROWS) - kChunk<KIND>), 0);
     }
-    static __device__ __forceinline__ uint32_t offset(size_t stride, size_t rows, int i)
+    static __device__ __forceinline__ uint32_t offset(size_t stride, size_t rows, int t, int i)
     {
-        const int r = TURNED ? row(i) - early(rows, i) + lower(rows) : (int)min((size_t)row(i), rows - 1);
-        const uint32_t step = (uint32_t)stride, d = depth(i);
+        const int r = TURNED ? row(t, i) - early(rows, t, i) + lower(rows) : (int)min((size_t)row(t, i), rows - 1);
+        const uint32_t step = (uint32_t)stride, d = depth(t, i);
         return (TURNED ? d * step + r : r * step + d) * (uint32_t)kWidth<KIND>;
     }
     // Chunk i of the last part of a tile of k, which begins at k0 and ends at `last`, loaded without a branch: from a place inside, and
     // moved up and cleared by settle().
-    static __device__ __forceinline__ u32x4 rest(const ConstRows& m, size_t row0, size_t k0, size_t rows, size_t last, int i)
+    static __device__ __forceinline__ u32x4 rest(const ConstRows& m, size_t row0, size_t k0, size_t rows, size_t last, int t, int i)
     {
-        const size_t k = min(k0 + depth(i), last - (TURNED ? 1 : kChunk<KIND>));
-        const size_t at = TURNED ? k * m.stride + row0 + row(i) - early(rows, i) : (row0 + min((size_t)row(i), rows - 1)) * m.stride + k;
+        const size_t k = min(k0 + depth(t, i), last - (TURNED ? 1 : kChunk<KIND>));
+        const size_t at = TURNED ? k * m.stride + row0 + row(t, i) - early(rows, t, i) : (row0 + min((size_t)row(t, i), rows - 1)) * m.stride + k;
         return *(const u32x4_a2*)((const char*)m.data + at * kWidth<KIND>);
     }
-    static __device__ __forceinline__ void settle(u32x4& q, size_t k0, size_t rows, size_t last, int i)
+    static __device__ __forceinline__ void settle(u32x4& q, size_t k0, size_t rows, size_t last, int t, int i)
     {
-        const ptrdiff_t behind = (ptrdiff_t)(k0 + depth(i)) - (ptrdiff_t)last;      // of its first k; 0 and more: nothing is there
-        move_up<KIND>(q, TURNED ? early(rows, i) & (kChunk<KIND> - 1) : (int)max(behind + kChunk<KIND>, (ptrdiff_t)0) & (kChunk<KIND> - 1));
+        const ptrdiff_t behind = (ptrdiff_t)(k0 + depth(t, i)) - (ptrdiff_t)last;      // of its first k; 0 and more: nothing is there
+        move_up<KIND>(q, TURNED ? early(rows, t, i) & (kChunk<KIND> - 1) : (int)max(behind + kChunk<KIND>, (ptrdiff_t)0) & (kChunk<KIND> - 1));
         if (behind >= 0) q = u32x4{};
     }
     static __device__ __forceinline__ const char* first(const ConstRows& m, size_t row0, size_t k0, size_t rows)
@@ -279,6 +279,10 @@ __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 :
     lds_char* const tile = (lds_char*)lds;
 
     for (unsigned i = blockIdx.x; i < g.units; i += gridDim.x) {
+        // Not known to be the same in every turn, so that what a lane derives from it is not kept, in memory, over the loop: us, kept /
+        // formed anew, input gradient 4096 x 20480 x 5120 664 / 637, weight gradient 8192 x 4096 x 16384 838 / 825.
+        int t = threadIdx.x;
+        asm volatile("" : "+v"(t));
         const Unit unit = unit_at(g, i);
         const Origin origin = origin_of(g, unit.tile);
         const size_t m0 = origin.m, n0 = origin.n, first = unit.first, last = unit.last;
@@ -302,12 +306,12 @@ __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 :
         };
         auto fetch = [&](u32x4 (&ra)[StageA::kCount], u32x4 (&rb)[StageB::kCount], size_t k0) {
             #pragma unroll
-            for (int c = 0; c < StageA::kCount; ++c) ra[c] = StageA::load(p.a, m0, k0, p.m, last, c);
+            for (int c = 0; c < StageA::kCount; ++c) ra[c] = StageA::load(p.a, m0, k0, p.m, last, t, c);
             #pragma unroll
-            for (int c = 0; c < StageB::kCount; ++c) rb[c] = StageB::load(p.b, n0, k0, p.n, last, c);
+            for (int c = 0; c < StageB::kCount; ++c) rb[c] = StageB::load(p.b, n0, k0, p.n, last, t, c);
         };
         auto put = [&](const u32x4 (&ra)[StageA::kCount], const u32x4 (&rb)[StageB::kCount], int at) {
-            lds_char* const to = tile + at * kTileBytes + threadIdx.x * 16;
+            lds_char* const to = tile + at * kTileBytes + t * 16;
             #pragma unroll
             for (int c = 0; c < StageA::kCount; ++c) *(__attribute__((address_space(3))) u32x4*)(to + c * kLanes * 16) = ra[c];
             #pragma unroll
@@ -318,13 +322,13 @@ __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 :
             if (const size_t rest = last > first ? (last - first) % kDepth<KIND> : 0) {      // in front: a sum has no order
                 u32x4 ra[StageA::kCount], rb[StageB::kCount];
                 #pragma unroll
-                for (int c = 0; c < StageA::kCount; ++c) ra[c] = StageA::rest(p.a, m0, last - rest, g.a_rows - m0, last, c);
+                for (int c = 0; c < StageA::kCount; ++c) ra[c] = StageA::rest(p.a, m0, last - rest, g.a_rows - m0, last, t, c);
                 #pragma unroll
-                for (int c = 0; c < StageB::kCount; ++c) rb[c] = StageB::rest(p.b, n0, last - rest, g.b_rows - n0, last, c);
+                for (int c = 0; c < StageB::kCount; ++c) rb[c] = StageB::rest(p.b, n0, last - rest, g.b_rows - n0, last, t, c);
                 #pragma unroll
-                for (int c = 0; c < StageA::kCount; ++c) StageA::settle(ra[c], last - rest, g.a_rows - m0, last, c);
+                for (int c = 0; c < StageA::kCount; ++c) StageA::settle(ra[c], last - rest, g.a_rows - m0, last, t, c);
                 #pragma unroll
-                for (int c = 0; c < StageB::kCount; ++c) StageB::settle(rb[c], last - rest, g.b_rows - n0, last, c);
+                for (int c = 0; c < StageB::kCount; ++c) StageB::settle(rb[c], last - rest, g.b_rows - n0, last, t, c);
                 put(ra, rb, 0);
                 __syncthreads();
                 #pragma unroll
@@ -340,9 +344,9 @@ __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 :
             if (whole) {
                 uint32_t oa[StageA::kCount], ob[StageB::kCount];
                 #pragma unroll
-                for (int c = 0; c < StageA::kCount; ++c) oa[c] = StageA::offset(p.a.stride, g.a_rows - m0, c);
+                for (int c = 0; c < StageA::kCount; ++c) oa[c] = StageA::offset(p.a.stride, g.a_rows - m0, t, c);
                 #pragma unroll
-                for (int c = 0; c < StageB::kCount; ++c) ob[c] = StageB::offset(p.b.stride, g.b_rows - n0, c);
+                for (int c = 0; c < StageB::kCount; ++c) ob[c] = StageB::offset(p.b.stride, g.b_rows - n0, t, c);
                 const char *from_a = StageA::first(p.a, m0, first, g.a_rows - m0), *from_b = StageB::first(p.b, n0, first, g.b_rows - n0);
                 const size_t step_a = StageA::step(p.a), step_b = StageB::step(p.b);
                 if constexpr (WAY == kThrough) {
@@ -358,11 +362,11 @@ __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 :
                     auto place = [&](int at) {
                         if (AT && p.m - m0 < BM) {              // the tile at the rows' end
                             #pragma unroll
-                            for (int c = 0; c < StageA::kCount; ++c) move_up<KIND>(ra[c], StageA::early(p.m - m0, c));
+                            for (int c = 0; c < StageA::kCount; ++c) move_up<KIND>(ra[c], StageA::early(p.m - m0, t, c));
                         }
                         if (BT && p.n - n0 < BN) {
                             #pragma unroll
-                            for (int c = 0; c < StageB::kCount; ++c) move_up<KIND>(rb[c], StageB::early(p.n - n0, c));
+                            for (int c = 0; c < StageB::kCount; ++c) move_up<KIND>(rb[c], StageB::early(p.n - n0, t, c));
                         }
                         put(ra, rb, at);
                     };
