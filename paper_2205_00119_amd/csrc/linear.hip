@@ -333,6 +333,7 @@ __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 :
                 __syncthreads();
                 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
+                    if (AT && rest <= half * (kDepth<KIND> / 2)) break;      // the gradient of a weight may have few rows
                     PieceA pa;
                     PieceB pb;
                     read(pa, pb, 0, half);
