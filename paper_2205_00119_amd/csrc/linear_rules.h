@@ -39,8 +39,8 @@ constexpr size_t copy_stride(size_t row, size_t width) { return ceil_div(row * w
 // slow: what a tile of k takes against operands on 16 bytes.  Measured (us): a tile of k for all workgroups that fit, 256 x 256, one on
 // a compute unit, 1.45 (4096 x 8192 x 4096 bf16 191), 128 x 128, two on one, 0.9 (2048 x 4096 x 4096 62.5), one on one 0.56
 // (4096 x 8192 x 1024 78); 320 tiles of 128 x 128 with k = 5120 63.5, in three parts each 71; beginning and end of a tile 5 and 3.5.
-// In 32 bits, of 128 x 128, two on one 3.66 (2048 x 4096 x 4096 468) and one on one 1.95, of 64 x 64 1.06 and 0.69 (input gradient
-// 154 x 5120 x 5120 in one part 113, in three 92; of 128 x 128 in three 118).
+// In 32 bits, of 128 x 128, two on one 3.66 (2048 x 4096 x 4096 468) and one on one 1.95, of 64 x 64 0.69 to 1.95 with one to four
+// (input gradient 154 x 5120 x 5120 in one part 113, in three 92; of 128 x 128 in three 118).
 struct TileCost {
     ProductPlan plan;
     double ns;
@@ -49,20 +49,18 @@ inline TileCost cost_of_tiles(const ProductShape& s, size_t tile, size_t room, d
 {
     const size_t tiles = ceil_div(s.m, tile) * ceil_div(s.n, tile), depths = ceil_div(s.k, 128 / s.width);
     const bool large = tile == 256;
-    double full = large ? 1450 : 900, half = large ? 1450 : 560, ends = large ? 5000 : 3500;
-    const size_t slots = large ? kCUs : 2 * kCUs;
-    if (s.width == 4) {
-        full = tile == 128 ? 3660 : 1060;
-        half = tile == 128 ? 1950 : 690;
-    }
-    full *= slow;
-    half *= slow;
+    const double ends = large ? 5000 : 3500;
+    const size_t slots = large ? kCUs : tile == 128 ? 2 * kCUs : 4 * kCUs;
+    // with one, two, three and four workgroups on a compute unit
+    const double four[4] = {690, 1060, 1500, 1950}, two[2] = {1950, 3660};
+    auto tile_of_k = [&](size_t units) {
+        if (large) return 1450 * slow;
+        if (s.width == 4) return (tile == 128 ? two : four)[ceil_div(units, kCUs) - 1] * slow;
+        return (units <= kCUs ? 560 : 662 + 238 * (double)(units - kCUs) / kCUs) * slow;       // what all share counts too
+    };
     auto rounds = [&](size_t units, size_t depth) {
         const size_t rest = units % slots;
-        double last = half;
-        // in 32 bits the matrix instructions of a compute unit with two workgroups decide, in 16 what all share does too
-        if (rest > kCUs) last += (full - half) * (s.width == 4 ? 1 : 0.3 + 0.7 * (double)(rest - kCUs) / kCUs);
-        return (units / slots) * (depth * full + ends) + (rest ? depth * last + ends : 0);
+        return (units / slots) * (depth * tile_of_k(slots) + ends) + (rest ? depth * tile_of_k(rest) + ends : 0);
     };
     TileCost best{{false, tile, tile, tiles, 0, 1, depths, 0, 0}, rounds(tiles, depths)};
     for (const size_t shared : {tiles % slots, tiles % slots + slots}) {
@@ -111,7 +109,7 @@ inline ProductPlan plan_product(const ProductShape& s)
     // gradients 107 / 86 and 103 / 80, 300 x 2047 x 5121 36.2 / 35.9; 256 x 256, 4095 x 3001 x 3003 107 / 83, 4095 x 8193 x 4095 256 / 254.
     // Both turned, 256 x 256 takes 1.8 times as long as on 16 bytes, and 128 x 128 is faster.  32-bit products are bound by the matrix
     // instructions.
-    const TileCost own = s.width == 4 ? best(kLinearWorkspace, 1.05, 0) : best(kLinearWorkspace, 1.6, s.a_turned ? 0 : 1.45);
+    const TileCost own = s.width == 4 ? best(kLinearWorkspace, 1.1, 0) : best(kLinearWorkspace, 1.6, s.a_turned ? 0 : 1.45);
     const size_t k = s.a_on_16 || s.b_on_16 ? s.k : copy_k(s.k, s.width);
     const size_t a = s.a_on_16 ? 0 : (s.a_turned ? k * copy_stride(s.m, s.width) : s.m * copy_stride(k, s.width)) * s.width;
     const size_t b = s.b_on_16 ? 0 : (s.b_turned ? k * copy_stride(s.n, s.width) : s.n * copy_stride(k, s.width)) * s.width;
