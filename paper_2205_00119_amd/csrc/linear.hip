@@ -72,7 +72,7 @@ template <int KIND> __device__ __forceinline__ void move_up(u32x4& q, int by)
 // How the lanes of a workgroup bring a tile of ROWS rows into the LDS: chunk i * LANES + t in the order of the places there, t: the lane.
 template <int KIND, bool TURNED, int ROWS, int LANES> struct Stage {
     static constexpr int kCount = ROWS * 8 / LANES, kAcross = ROWS * (int)kWidth<KIND> / 16;
-    static_assert(ROWS * 8 % LANES == 0, "");
+    static_assert(ROWS * 8 % LANES == 0 && (!TURNED || kAcross >= 16), "whole rounds of lanes, and places that stay in their row");
     // row (turned: first of the rows) and k (first of them; turned: the k) of the tile that chunk i holds
     static __device__ __forceinline__ int row(int t, int i)
     {
@@ -719,9 +719,9 @@ template <int KIND> __global__ __launch_bounds__(kCopyLanes) void copy_kernel(Co
     }
 }
 
-template <int KIND, bool AT, bool BT, int TILE, int WM, int WN, int WAY> int launch_tiles(const ProductArgs& g, void* stream)
+template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN, int WAY> int launch_tiles(const ProductArgs& g, void* stream)
 {
-    return launch_args(product_kernel<KIND, AT, BT, TILE, TILE, WM, WN, WAY>, dim3(grid_of(g.units)), dim3(64 * WM * WN), 0, stream, g);
+    return launch_args(product_kernel<KIND, AT, BT, BM, BN, WM, WN, WAY>, dim3(grid_of(g.units)), dim3(64 * WM * WN), 0, stream, g);
 }
 
 }  // namespace
@@ -765,14 +765,16 @@ int launch_product(const Product& p, const ProductPlan& plan, int kind, void* st
             if constexpr (!AT)
                 if (plan.few) return launch_few<KIND, BT>(g, stream);
             if (!in_chunks(p.a, AT, p.m, p.k, W) || !in_chunks(p.b, BT, p.n, p.k, W))
-                return launch_tiles<KIND, AT, BT, 128, 2, 2, kGuarded>(g, stream);
+                return launch_tiles<KIND, AT, BT, 128, 128, 2, 2, kGuarded>(g, stream);
             return dispatch_flag(on_16(g.p.a, AT, g.a_rows, W) && on_16(g.p.b, BT, g.b_rows, W), [&](auto D) {
                 constexpr int WAY = decltype(D)::value ? kDirect : kThrough;
+                if constexpr (KIND == kF32 && !AT)
+                    if (plan.bm == 32) return launch_tiles<KIND, AT, BT, 32, 128, 2, 2, WAY>(g, stream);
                 if constexpr (KIND == kF32)
-                    if (plan.bm == 64) return launch_tiles<KIND, AT, BT, 64, 4, 1, WAY>(g, stream);
+                    if (plan.bm == 64) return launch_tiles<KIND, AT, BT, 64, 64, 4, 1, WAY>(g, stream);
                 if constexpr (KIND != kF32 && !(AT && WAY == kThrough))
-                    if (plan.bm == 256) return launch_tiles<KIND, AT, BT, 256, 2, 4, WAY>(g, stream);
-                return launch_tiles<KIND, AT, BT, 128, 2, 2, WAY>(g, stream);
+                    if (plan.bm == 256) return launch_tiles<KIND, AT, BT, 256, 256, 2, 4, WAY>(g, stream);
+                return launch_tiles<KIND, AT, BT, 128, 128, 2, 2, WAY>(g, stream);
             });
         }
     }); }); });

@@ -40,38 +40,38 @@ constexpr size_t copy_stride(size_t row, size_t width) { return ceil_div(row * w
 // a compute unit, 1.45 (4096 x 8192 x 4096 bf16 191), 128 x 128, two on one, 0.9 (2048 x 4096 x 4096 62.5), one on one 0.56
 // (4096 x 8192 x 1024 78); 320 tiles of 128 x 128 with k = 5120 63.5, in three parts each 71; beginning and end of a tile 5 and 3.5.
 // In 32 bits, of 128 x 128, two on one 3.66 (2048 x 4096 x 4096 468) and one on one 1.95, of 64 x 64 0.69 to 1.95 with one to four
-// (input gradient 154 x 5120 x 5120 in one part 113, in three 92; of 128 x 128 in three 118).
+// (input gradient 154 x 5120 x 5120 in one part 113, in three 92; of 128 x 128 in three 118), of 32 x 128 as much (in five 75).
 struct TileCost {
     ProductPlan plan;
     double ns;
 };
-inline TileCost cost_of_tiles(const ProductShape& s, size_t tile, size_t room, double slow)
+inline TileCost cost_of_tiles(const ProductShape& s, size_t bm, size_t bn, size_t room, double slow)
 {
-    const size_t tiles = ceil_div(s.m, tile) * ceil_div(s.n, tile), depths = ceil_div(s.k, 128 / s.width);
-    const bool large = tile == 256;
+    const size_t tiles = ceil_div(s.m, bm) * ceil_div(s.n, bn), size = bm * bn, depths = ceil_div(s.k, 128 / s.width);
+    const bool large = bm == 256, small = bm < 128;
     const double ends = large ? 5000 : 3500;
-    const size_t slots = large ? kCUs : tile == 128 ? 2 * kCUs : 4 * kCUs;
+    const size_t slots = large ? kCUs : small ? 4 * kCUs : 2 * kCUs;
     // with one, two, three and four workgroups on a compute unit
     const double four[4] = {690, 1060, 1500, 1950}, two[2] = {1950, 3660};
     auto tile_of_k = [&](size_t units) {
         if (large) return 1450 * slow;
-        if (s.width == 4) return (tile == 128 ? two : four)[ceil_div(units, kCUs) - 1] * slow;
+        if (s.width == 4) return (small ? four : two)[ceil_div(units, kCUs) - 1] * slow;
         return (units <= kCUs ? 560 : 662 + 238 * (double)(units - kCUs) / kCUs) * slow;       // what all share counts too
     };
     auto rounds = [&](size_t units, size_t depth) {
         const size_t rest = units % slots;
         return (units / slots) * (depth * tile_of_k(slots) + ends) + (rest ? depth * tile_of_k(rest) + ends : 0);
     };
-    TileCost best{{false, tile, tile, tiles, 0, 1, depths, 0, 0}, rounds(tiles, depths)};
+    TileCost best{{false, bm, bn, tiles, 0, 1, depths, 0, 0}, rounds(tiles, depths)};
     for (const size_t shared : {tiles % slots, tiles % slots + slots}) {
         if (shared == 0 || shared > tiles) continue;
         for (size_t splits = 2; splits <= 64 && splits <= depths; ++splits) {
             const size_t units = shared * splits, depth = ceil_div(depths, splits);
-            if (units > 2 * slots || units * tile * tile * 4 > room) break;
+            if (units > 2 * slots || units * size * 4 > room) break;
             if (ceil_div(depths, depth) < splits) continue;
             // the parts are written and read, and a second launch
-            const double ns = rounds(tiles - shared, depths) + rounds(units, depth) + units * tile * tile * 8 / 5000.0 + 5000;
-            if (ns < best.ns) best = {{false, tile, tile, tiles - shared, shared, splits, depth, 0, 0}, ns};
+            const double ns = rounds(tiles - shared, depths) + rounds(units, depth) + units * size * 8 / 5000.0 + 5000;
+            if (ns < best.ns) best = {{false, bm, bn, tiles - shared, shared, splits, depth, 0, 0}, ns};
         }
     }
     return best;
@@ -94,13 +94,17 @@ inline ProductPlan plan_product(const ProductShape& s)
         return {true, bm, bn, splits > 1 ? 0 : tiles, splits > 1 ? tiles : 0, splits, depth, 0, 0};
     }
     auto best = [&](size_t room, double slow_128, double slow_256) {           // 0: no tiles of 256 x 256
-        const TileCost small = cost_of_tiles(s, 128, room, slow_128);
-        if (s.width == 4 && s.chunks) {                    // narrower tiles, since idle rows and columns cost as much as others
-            const TileCost tiny = cost_of_tiles(s, 64, room, slow_128);
-            return tiny.ns < small.ns ? tiny : small;
+        TileCost small = cost_of_tiles(s, 128, 128, room, slow_128);
+        if (s.width == 4 && s.chunks) {                    // smaller tiles, since idle rows and columns cost as much as others
+            for (const size_t bm : {64, 32}) {
+                if (bm == 32 && s.a_turned) continue;      // its swizzle takes rows of 64
+                const TileCost other = cost_of_tiles(s, bm, 4096 / bm, room, slow_128);
+                if (other.ns < small.ns) small = other;
+            }
+            return small;
         }
         if (!s.chunks || slow_256 == 0) return small;
-        const TileCost large = cost_of_tiles(s, 256, room, slow_256);
+        const TileCost large = cost_of_tiles(s, 256, 256, room, slow_256);
         return large.ns <= small.ns ? large : small;
     };
     const bool off = s.chunks && !(s.a_on_16 && s.b_on_16);

@@ -53,7 +53,10 @@ def test_every_tile_and_every_k_is_taken_once(plan):
             assert turned[1] or b16, what
             assert not blocks or turned[1] or p["bn"] == 64, what
         else:
-            assert p["bm"] == p["bn"] in (64, 128, 256) and (p["bm"] == 128 or (chunks and (p["bm"] == 256) == (width == 2))), what
+            tile = p["bm"], p["bn"]
+            assert tile == (128, 128) or chunks, what
+            assert tile in [(128, 128)] + ([(256, 256)] if width == 2 else [(64, 64), (32, 128)]), what
+            assert tile != (32, 128) or not turned[0], what
         copied = [p["a_copy"], p["b_copy"]]
         assert (not copied[0] or not a16) and (not copied[1] or not b16) and (chunks or copied == [0, 0]), what
         if any(copied):                                                                # all that is off 16 bytes
@@ -87,6 +90,7 @@ def test_sizes_of_the_gpu_tests_reach_every_kernel(plan):
     for op in ("linear", "input", "weight"):
         wanted += [(op, w, how, 128, 0) for w in (2, 4) for how in ("guarded", "direct", "through")]
         wanted += [(op, 4, how, 64, 0) for how in ("direct", "through")]
+        wanted += [x for how in ("direct", "through") for x in ((op, 4, how, 32, 0), (op, 4, how, 32, "parts", False)) if op != "weight"]
         wanted += [(op, 2, how, 256, 0) for how in ("direct", "through") if (op, how) != ("weight", "through")]
         wanted += [(op, w, how, bm, "parts", False) for w, bm in ((2, 128), (4, 64)) for how in ("direct", "through")]
         wanted += [(op, 2, "copy")]
