@@ -86,8 +86,12 @@ inline ProductPlan plan_product(const ProductShape& s)
         const size_t bn = s.b_turned ? 256 / s.width : s.blocks ? 64 : 16;
         const size_t tiles = ceil_div(s.n, bn);
         size_t splits = 1, depth = depths;
-        if (s.b_turned && tiles < 2 * kCUs) {              // few columns: enough workgroups for the memory's latency
-            splits = std::min(2 * kCUs / tiles, ceil_div(depths, 8));
+        // Few columns: enough workgroups for the memory's latency.  us, one part / several, 16 rows: 16384 x 1024 bf16 30.6 / 13.3,
+        // 20480 x 5120 72 / 49, 16384 x 1 20 / 7.3, 2560 x 256 f32 11.5 / 7.5.  Of shorter k, or with a workgroup for every compute unit,
+        // the join takes what that saves: 5120 x 2560 bf16 11.5 / 12.5, 8192 x 4096 17.1 / 19.7.
+        if (tiles < 2 * kCUs && (s.b_turned || depths >= (tiles < kCUs ? 256 / s.width : 320))) {
+            splits = s.b_turned ? std::min(2 * kCUs / tiles, ceil_div(depths, 8))
+                                : std::min({std::max<size_t>(ceil_div(2 * kCUs, tiles), 4), ceil_div(depths, 16), size_t{32}});
             depth = ceil_div(depths, splits);
             splits = ceil_div(depths, depth);
         }

@@ -95,7 +95,7 @@ def test_sizes_of_the_gpu_tests_reach_every_kernel(plan):
         wanted += [(op, w, how, bm, "parts", False) for w, bm in ((2, 128), (4, 64)) for how in ("direct", "through")]
         wanted += [(op, 2, "copy")]
     wanted += [("input", w, "few", bm, 256 // w) for w in (2, 4) for bm in (16, 32)]
-    wanted += [("input", w, "few", bm, "parts", False) for w in (2, 4) for bm in (16, 32)]
+    wanted += [(op, w, "few", bm, "parts", False) for op in ("linear", "input") for w in (2, 4) for bm in (16, 32)]
     wanted += [("linear", w, "few", bm, bn) for w in (2, 4) for bm in (16, 32) for bn in (16, 64)]
     # whole tiles and shared ones in one launch
     wanted += [("linear", 2, "direct", bm, "parts", True) for bm in (128, 256)]
