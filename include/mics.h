@@ -50,9 +50,9 @@
  *     coalesced ones, which issue one per 48 to 96 tensors, backward passes
  *     that sum over rows (one with few rows or none, else two, and one more
  *     with rows of more than 8192 columns), log probabilities of few long
- *     rows (two) and products whose last tiles are shared or whose operands
- *     are copied first (one more each): these may have enqueued earlier
- *     launches when a later one fails.
+ *     rows (two) and products of which several workgroups share a tile or
+ *     whose operands are copied first (one more each): these may have
+ *     enqueued earlier launches when a later one fails.
  *   - Return value: MICS_OK or a negative MICS_ERR_*; mics_last_error() gives
  *     the text for the calling thread's most recent failure.
  *   - bf16 values travel as uint16_t bit patterns (upper half of a binary32).
