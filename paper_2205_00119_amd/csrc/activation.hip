@@ -12,8 +12,8 @@ namespace {
 
 // A wavefront takes a stripe of 64 vectors of a row, or 64 >> shift narrow rows, and goes down the rows, FLIGHT of them at a time:
 // places come from shifts alone and the bias is loaded once.  Workgroups that follow one another take a row's
-// stripes, not rows: memory is slower where they
-// take rows (us, 4096 x 10240 bf16 tanh 40.3 / 46.8), and where wavefronts go down many rows (4096 x 32768 115 / 128).
+// stripes, not rows: memory is slower where they take rows (us, 4096 x 10240 bf16 tanh 40.3 / 46.8), and where wavefronts go down many
+// rows (4096 x 32768 115 / 128).
 constexpr size_t kMostDown = 65535;            // workgroups above one another
 template <int FLIGHT> struct Down {
     static constexpr int kLanes = FLIGHT == 1 ? 256 : 64;

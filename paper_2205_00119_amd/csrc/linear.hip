@@ -249,7 +249,6 @@ __device__ __forceinline__ Unit unit_at(const ProductArgs& g, unsigned i)
     return {g.whole + at, first, min(g.p.k, first + g.depth), g.p.parts + ((size_t)at * g.splits + split) * (g.bm * g.bn)};
 }
 
-
 // One workgroup for a tile of BM x BN results, WM x WN wavefronts with 64 columns each.
 // WAY kDirect: whole chunks begin on 16 bytes, so tiles of k go straight into the LDS, the next one and the one behind it on their
 // way; while a wavefront multiplies one half of a tile it reads the next half.  Reads and loads are spread among the matrix
@@ -260,7 +259,6 @@ __device__ __forceinline__ Unit unit_at(const ProductArgs& g, unsigned i)
 // 32 x 32 (830 / 919), and four wavefronts of 128 x 128 (823 / 887).
 // kThrough: chunks begin on any element; a tile waits in registers while the one before is multiplied.
 // kGuarded: rows shorter than a chunk, tiles of more than 2^31 bytes; every chunk is looked at.
-
 enum { kDirect, kThrough, kGuarded };
 template <int KIND, bool AT, bool BT, int BM, int BN, int WM, int WN, int WAY>
 __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 : 1) void product_kernel(ProductArgs g)
