@@ -452,8 +452,9 @@ int mics_token_logprobs_backward(void* dlogits, const void* logits, const int64_
  * own) and `scales` (fp32, packed): every row is cut into blocks of MICS_CHECKPOINT_BLOCK columns, the last one shorter, and
  * scales[row * ceil(cols / 64) + b] belongs to block b.  In binary32, each operation rounded to nearest even, for every block
  *     top = max(max |z|, 2^-100),   scale = top / 127,   code = rint(z * (127 / top)),
- * and an element stands for code * scale: it is off by at most half a scale and the roundings.  A block that holds an
- * infinity or NaN has the scale NaN and codes of 0: all of it stands for NaN.
+ * and an element stands for code * scale: it is off by at most half a scale and the roundings.  (127 scales of a block whose largest is
+ * the largest finite binary32 number round to infinity, which that element then stands for; no other does.)  A block that holds
+ * an infinity or NaN has the scale NaN and codes of 0: all of it stands for NaN.
  * mics_checkpoint_scales: rows * ceil(cols / 64), the number of scales; 0 on bad arguments.
  */
 #define MICS_CHECKPOINT_BLOCK 64

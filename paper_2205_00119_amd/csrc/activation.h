@@ -105,13 +105,14 @@ __device__ __forceinline__ uint32_t codes_of(const float* z, const Coding& c)
     const uint32_t high = __builtin_amdgcn_perm(code_of(z[3], c.by), code_of(z[2], c.by), 0x0C0C0400u);
     return __builtin_amdgcn_perm(high, low, 0x05040100u) & c.keep;
 }
-// What four codes stand for: of code + 128, times the scale, 128 scales are taken away, which rounds once as code * scale does.
+// What four codes stand for: code * scale, rounded once.  Signed bytes are converted where they lie (v_cvt_f32_i32 of a byte of its
+// operand), two operations an element, and none gives more than the result: 128 scales of a block at the end of the range are infinite.
+// us against a biased conversion whose 128 scales are taken away in a fused multiply: 4096 x 32768 bf16 read with tanh 80.9 / 83.4,
+// with gelu 103 / 108, backward the same.
 __device__ __forceinline__ void restored(uint32_t codes, float scale, float* v)
 {
-    const uint32_t u = codes ^ 0x80808080u;
-    const float off = -128.f * scale;
     #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __builtin_fmaf((float)(uint8_t)(u >> (8 * i)), scale, off);
+    for (int i = 0; i < 4; ++i) v[i] = (float)(int8_t)(codes >> (8 * i)) * scale;
 }
 
 typedef u32x2 u32x2_a1 __attribute__((aligned(1)));
