@@ -487,7 +487,7 @@ __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 :
                 for (int n = 0; n < TN; ++n)
                     *(lds_f4*)(mine + ((m * 16 + lane % 16) * kStagePitch + n * 16 + lane / 16 * 4) * 4) = acc[part * kOut + m][n];
             }
-            // its own LDS accesses are in order
+            wave_lds_order();                                   // other lanes' sums are read
             const size_t row0 = m0 + wm * TM * 16 + part * kOut * 16 + lane / kAcross;
             const int rows = row0 < p.m ? (int)min((p.m - row0 + kStep - 1) / kStep, (size_t)(kOut * 16 / kStep)) : 0;
             const lds_char* from = mine + (lane / kAcross * kStagePitch + lane % kAcross * kVec) * 4;
@@ -521,6 +521,7 @@ __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 :
                     finish<KIND>(e, row0 + r * kStep, (unsigned)(col / kVec), (unsigned)p.n, valid, v);
                 }
             }
+            wave_lds_order();                                   // before the next part takes their place
         }
         __syncthreads();
     }

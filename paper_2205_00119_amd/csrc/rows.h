@@ -300,6 +300,15 @@ __device__ __forceinline__ void barrier_lds()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// Orders LDS accesses of one wavefront's lanes before and after it.  They complete in program order, so this is no
+// instruction: it tells the compiler, to whom the lanes' addresses do not alias, to keep that order.
+__device__ __forceinline__ void wave_lds_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // Lanes are summed in a fixed order within rows of 16 by shifts, then across them; the result is in every lane.
 template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_zero(float v)
 {
