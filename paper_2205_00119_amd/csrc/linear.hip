@@ -129,11 +129,15 @@ template <int KIND, bool TURNED, int ROWS, int LANES> struct Stage {
 };
 
 // 16 bytes for each lane from `base` + `offset` into the LDS from byte `to` + TO on, lane after lane.  It counts as a load in flight that
-// the compiler does not know of: landed() waits.  m0, which nothing else here uses, has to settle first.
+// the compiler does not know of: landed() waits.  m0, which the LDS address goes through, has to settle first.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"        // that no value is kept in m0, which is reserved, is what is meant
 template <int TO> __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(base), "v"(offset), "s"(to), "i"(TO) : "memory", "scc");
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(base), "v"(offset), "s"(to), "i"(TO)
+                 : "memory", "scc", "m0");
 }
+#pragma clang diagnostic pop
 // f(std::integral_constant<int, i>) for every i below N.
 template <int... I, typename F> __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f)
 {

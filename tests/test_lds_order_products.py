@@ -12,8 +12,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
-def kernels(tmp_path_factory):
-    """name -> accesses to the LDS: W stores of floats, w other stores, r loads, | fences."""
+def ir(tmp_path_factory):
     spec = importlib.util.spec_from_file_location("lib_build", os.path.join(ROOT, "paper_2205_00119_amd", "build.py"))
     lib_build = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(lib_build)
@@ -23,8 +22,14 @@ def kernels(tmp_path_factory):
     flags = [f for f in lib_build.FLAGS if f not in ("-shared", "-fPIC")]
     subprocess.run([lib_build.HIPCC, *flags, "--offload-device-only", "-S", "-emit-llvm", "-o", out,
                     os.path.join(ROOT, "paper_2205_00119_amd", "csrc", "linear.hip")], check=True, capture_output=True)
+    return open(out).read().splitlines()
+
+
+@pytest.fixture(scope="module")
+def kernels(ir):
+    """name -> accesses to the LDS: W stores of floats, w other stores, r loads, | fences."""
     found, accesses = {}, None
-    for line in open(out):
+    for line in ir:
         start = re.match(r"define .*@(\S+?)\(", line)
         if start:
             accesses = found.setdefault(start.group(1), [])
@@ -50,3 +55,9 @@ def test_results_pass_through_the_lds_in_an_order_that_the_compiler_knows(kernel
         assert re.fullmatch(r"(W+\|r+\|)+", order), (name, order)
         parts.add(len(re.findall("W+", order)))
     assert parts == {1, 2}                                       # tiles of 256 rows come in two parts
+
+
+def test_assembly_that_sets_m0_says_so(ir):
+    """A value that the compiler holds in m0, as it does for some LDS and message instructions, is then not taken to be there still."""
+    sets = [line for line in ir if re.search(r'asm sideeffect "[^"]*\bm0\b', line)]
+    assert sets and all("~{m0}" in line for line in sets)
