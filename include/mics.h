@@ -493,8 +493,9 @@ int mics_activation_backward(void* dx, void* dbias, const void* dy, const void* 
  * The linear layer.  x: rows rows of in_features, weight: out_features rows of in_features, both of `dtype`;
  *     z = x weight^T + bias,   out = residual + act(z)
  * and for the backward pass pre = z in `dtype`, or codes, scales = its checkpoint.  The act, the residual and the checkpoint take
- * z before it is rounded.  Products of 16-bit elements are exact and summed in binary32 in an order that depends on sizes,
- * strides and alignment alone.
+ * z before it is rounded.  Products of 16-bit elements are exact and summed in binary32 in an order that depends on sizes, dtype,
+ * strides and the operands' alignment to 16 bytes, up to 32 rows also on whether there are codes, and on nothing else: up to 32 rows a pass
+ * that keeps a checkpoint and one that does not may differ in the last bits of the sums.
  *   strides          out, pre, codes, x, weight, residual
  *   pre              may be NULL
  *   codes, scales    of out_features columns; may be NULL, both or neither
