@@ -300,7 +300,8 @@ int mics_reduce_scatter_accum_coalesced_typed(float* acc, const void* const* gra
  *   - A result matrix may be an input matrix of the same address and stride.  Matrices of one stride may
  *     lie between each other's rows.  No other overlap of a result is allowed (checked).
  *   - Everything is computed in binary32 and rounded to nearest even once, when it is stored.
- *     Sums are formed in an order that depends on the sizes alone: results are reproducible.
+ *     Sums are formed in an order that depends on the sizes and dtype alone (the linear layer's on what is said there): results are
+ *     reproducible.
  *   - `workspace`: caller-owned scratch of at least the stated bytes, 8-byte aligned, its contents of no
  *     meaning before or after; one may serve any number of calls that are ordered by a stream.
  */

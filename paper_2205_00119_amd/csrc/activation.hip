@@ -34,7 +34,8 @@ template <int FLIGHT> struct Down {
     __device__ __forceinline__ unsigned across() const { return 64u >> shift; }
 };
 // Memory bounds it where operations do not: an element has some 30 of them for the 5.06 bytes that it moves in 16 bits (4096 x 32768
-// bf16 tanh 116 to 121 us, 5.6 to 5.9 TB/s; gelu, whose polynomial takes ten more, 131 to 141).
+// bf16 tanh 121 us, 5.6 TB/s; gelu, whose polynomial takes ten more, 148 to 151; runs of calls on two sets of matrices in turn, from
+// event to event: a kernel trace has medians a fifth above that and the same minima).
 template <int FLIGHT> struct ActivationArgs {
     ActivationPass a;
     Down<FLIGHT> down;
@@ -66,7 +67,7 @@ template <int KIND, int FLIGHT> __global__ __launch_bounds__(Down<FLIGHT>::kLane
     }
 }
 
-// 3.06 bytes for some 18 operations with an activation (4096 x 32768 bf16 tanh 78 to 84 us, 4.9 to 5.3 TB/s, gelu 100 to 108).
+// 3.06 bytes for some 18 operations with an activation (4096 x 32768 bf16 tanh 81 us, 5.1 TB/s, gelu 103, measured as above).
 template <int FLIGHT> struct ReadArgs {
     CheckpointRead a;
     Down<FLIGHT> down;
@@ -104,7 +105,7 @@ template <int KIND, int FLIGHT> __global__ __launch_bounds__(Down<FLIGHT>::kLane
 
 // dx and, with dbias, column sums over the rows of a workgroup: a wavefront takes a stripe of 64 vectors, or 64 >> shift narrow
 // rows, and every gridDim.y * kBackWaves-th set of rows, ROWS of them in flight.  Bound by memory (4096 x 32768 bf16 tanh 137 us,
-// 4.95 TB/s; without sums 123, 5.5) and, in small calls, by the second launch, which joins the sums.
+// 4.95 TB/s; without sums 119 to 125, 5.4 to 5.7) and, in small calls, by the second launch, which joins the sums.
 constexpr int kBackWaves = 4;
 struct BackwardArgs {
     ActivationBackward a;

@@ -335,7 +335,7 @@ __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 :
                 __syncthreads();
                 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    if (AT && rest <= half * (kDepth<KIND> / 2)) break;      // the gradient of a weight may have few rows
+                    if (AT && rest <= (size_t)half * (kDepth<KIND> / 2)) break;      // the gradient of a weight may have few rows
                     PieceA pa;
                     PieceB pb;
                     read(pa, pb, 0, half);
@@ -537,8 +537,12 @@ __global__ __launch_bounds__(64 * WM * WN, WAY == kThrough && WM * WN == 4 ? 2 :
 //   b not turned   16 columns to an instruction, lane i of 16 has chunk lane / 16 of row i;
 //   b turned       a lane has a chunk of columns of kChunk k, which it turns around in registers: instruction j takes column j of
 //                  every chunk.
-// us, in tiles of 128 rows / so: 1 x 2560 x 10240 bf16 16.6 / 12.1 (the weights alone take 7.8, a launch 4), 1 x 10240 x 2560 22.3 / 14.5,
-// 16 x 2560 x 10240 f32 63.7 / 31.3, its input's gradient 65.8 / 22.4; 8 x 5120 x 20480 36.4 / 39.4, where tiles have enough to do.
+// us, in tiles of 32 to 128 rows, with parts of k / so, two sets of weights in turn: 1 x 2560 x 10240 bf16 17.4 / 12.0 (12 in the kernel's
+// own trace; the weights alone take 7.7), 1 x 4096 x 4096 12.9 / 7.9, 16 x 4096 x 4096 13.6 / 10.1, 32 x 4096 x 4096 14.2 / 13.5, the
+// input's gradient of 16 x 2560 x 10240 f32 25.6 / 22.5.  Every wavefront loads a for itself, once for every 16 columns, so tiles are
+// faster where rows and columns are many, and the rule, which takes this kernel for all it can serve, loses there: 16 x 5120 x 20480
+// bf16 47.7 / 61.0, 32 x 5120 x 20480 49.2 / 75.3, 8 x 2560 x 10240 f32 23.9 / 25.3, 32 x 20480 x 5120 f32 88.0 / 186, input's gradient
+// 32 x 2560 x 10240 f32 26.4 / 32.8.
 // Rows of b off 16 bytes are left to the tiles unless b is turned: 16 rows at a time from 64 bytes each, 56 / 150.  Two tiles of k at a
 // time and 32 or 64 columns were slower (39 / 51).
 constexpr int kFewWaves = 8;

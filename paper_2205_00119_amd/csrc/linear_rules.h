@@ -1,4 +1,5 @@
-// How a product is cut into tiles and parts: rules on sizes, strides and alignment, host code.
+// How a product is cut into tiles and parts: rules on sizes, an element's width, strides, alignment and whether blocks of a checkpoint
+// have to stay whole, host code.
 #pragma once
 
 #include <algorithm>
@@ -41,6 +42,8 @@ constexpr size_t copy_stride(size_t row, size_t width) { return ceil_div(row * w
 // (4096 x 8192 x 1024 78); 320 tiles of 128 x 128 with k = 5120 63.5, in three parts each 71; beginning and end of a tile 5 and 3.5.
 // In 32 bits, of 128 x 128, two on one 3.66 (2048 x 4096 x 4096 468) and one on one 1.95, of 64 x 64 0.69 to 1.95 with one to four
 // (input gradient 154 x 5120 x 5120 in one part 113, in three 92; of 128 x 128 in three 118), of 32 x 128 as much (in five 75).
+// The ends are one figure whatever is stored, which is too little where results of 32 bits end a short sum of 16-bit elements: weight
+// gradient 1003 x 2563 x 1285 off 16 bytes 18 by this, 25.8 measured.
 struct TileCost {
     ProductPlan plan;
     double ns;
@@ -88,7 +91,11 @@ inline ProductPlan plan_product(const ProductShape& s)
         size_t splits = 1, depth = depths;
         // Few columns: enough workgroups for the memory's latency.  us, one part / several, 16 rows: 16384 x 1024 bf16 30.6 / 13.3,
         // 20480 x 5120 72 / 49, 16384 x 1 20 / 7.3, 2560 x 256 f32 11.5 / 7.5.  Of shorter k, or with a workgroup for every compute unit,
-        // the join takes what that saves: 5120 x 2560 bf16 11.5 / 12.5, 8192 x 4096 17.1 / 19.7.
+        // the join takes what that saves: 5120 x 2560 bf16 11.5 / 12.5, 8192 x 4096 17.1 / 19.7, 16384 x 4096 31.3 / 34.5 (256 tiles of k;
+        // the line of 320 is between this and 20480 x 5120), 4096 x 4096 f32 19.6 / 20.0; 16384 x 4096 f32 88.9 / 83.3 is above it.
+        // Workgroups of 64 columns are a quarter as many, and parts would pay from shorter k on than these lines, measured with 16
+        // columns, let them: with a checkpoint 16 x 5120 x 2560 bf16 25.8 / 12.5, 16 x 4096 x 4096 20.9 / 13.4; where the lines do,
+        // 16 x 8192 x 4096 38.1 / 20.5, 16 x 16384 x 1024 72 / 13.5, 16 x 10240 x 2560 f32 91 / 32.6; 16 x 2560 x 10240 15.6 / 21.0.
         if (tiles < 2 * kCUs && (s.b_turned || depths >= (tiles < kCUs ? 256 / s.width : 320))) {
             splits = s.b_turned ? std::min(2 * kCUs / tiles, ceil_div(depths, 8))
                                 : std::min({std::max<size_t>(ceil_div(2 * kCUs, tiles), 4), ceil_div(depths, 16), size_t{32}});
